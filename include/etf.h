@@ -494,6 +494,92 @@ int64_t etf_ivf_workspace_bytes(const etf_ctx *ctx, int64_t Q, int k, int w);
 int etf_ivf_search(etf_ctx *ctx, const float *queries, int64_t Q, int k, int w, int32_t *out_ids, float *out_dist,
                    void *ws, int64_t ws_bytes);
 
+/* ---- attention over a cache in 8 bits ----------------------------------- */
+
+/* A language model's attention cache is a database like the others here: uncompressed queries against compressed
+ * vectors, scalar products, lists picked by a cheap score; it grows while the model answers, and what comes back is the
+ * softmax-weighted mean of the values instead of the nearest ids.  The cache is a set of device arrays that the caller
+ * owns and describes by an etf_kv_cache; the calls keep nothing between them.
+ *
+ * Tokens are held in blocks of ETF_KV_BLOCK, block j of a (sequence, head) = its tokens [64 j, 64 j + 64).  Full blocks lie
+ * in pages of a pool: e4m3 codes (OCP: 448 largest, 0x7F not a number), one scale for the block's keys and one for its values,
+ * each the smallest power of two s (2^-126 to 2^119) with amax <= 448 s; code = x / s rounded to the nearest, ties to even
+ * (448 in size at most).
+ * A power of two makes every multiplication by a scale exact and costs no precision, since the codes have exponents of
+ * their own.  The open block, the one that is not full yet, is kept in the queries' type and becomes codes once, when
+ * it is full: what a cache holds does not depend on the pieces in which its tokens came.
+ *   k       u8 [pages][64][head_dim]                 key codes
+ *   v       u8 [pages][head_dim][64]                 value codes, a row for each dimension
+ *   scales  float [pages][2]                         of the keys, of the values
+ *   bounds  u8 [pages][2][head_dim]                  smallest and largest key code of each dimension
+ *   tail_k  16-bit [batch][heads][2][64][head_dim]   open blocks: block j of sequence b in buffer (j + evicted[b]) % 2
+ *   tail_v  16-bit [batch][heads][2][head_dim][64]
+ *   table   i32 [batch][heads][max_blocks]           page of every full block.  An entry that is no page (negative, or too
+ *                                                    large) is a block that is not there: nothing is written to it, and
+ *                                                    attention and selection pass over it
+ *   lens    i32 [batch]                              tokens in each sequence's cache, the same for all its heads; counts as 0
+ *                                                    below that and as 64 max_blocks + 63 above that
+ *   evicted i32 [batch]                              blocks that etf_kv_evict has taken out of each sequence so far
+ * A page belongs to one block of one head.  batch * heads * max_blocks < 2^31; head_dim is 64, 96 or 128; all arrays
+ * 16-byte aligned.  lens is advanced by the caller (after etf_kv_append, before etf_kv_attend with the new tokens'
+ * queries); it may be taken back to no less than what the full blocks hold.
+ *
+ * Rows of k, v and q ([batch][n][heads or heads_q][head_dim], 16-bit) lie at strides[0..2] = elements from one sequence,
+ * token and head to the next, multiples of 8 (a NULL pointer: dense); a row is contiguous and 16-byte aligned.  counts
+ * (i32 [batch], device; NULL: all n) is how many of the n tokens each sequence has, the first ones.  Query head x
+ * reads key/value head x / (heads_q / heads).
+ * Query token i of a sequence is token lens - counts + i of its cache and sees the tokens up to itself.  Padding
+ * and tokens that see nothing get zeros and a logarithm of -inf. */
+#define ETF_KV_BLOCK 64      /* tokens of a block */
+#define ETF_KV_MAX_LIST 4096 /* largest w */
+enum { ETF_KV_BF16 = 0, ETF_KV_FP16 = 1 };  /* type of queries, new tokens, outputs and open blocks */
+typedef struct etf_kv_cache {
+    int32_t dtype, batch, heads, head_dim, max_blocks, pages;
+    void *k, *v, *bounds;
+    float *scales;
+    void *tail_k, *tail_v;
+    int32_t *table, *lens, *evicted;
+} etf_kv_cache;
+
+/* Writes the new tokens at [lens, lens + counts) of every sequence: into the open block, and as codes into the pages of the
+ * blocks that they complete, for which table must have entries; lens stays as it is.  Tokens past the table's end are
+ * dropped.  A token with a key or value that is not finite is kept with keys that are not numbers and values of zero:
+ * rows that see it become not a number, no others do, and its block's scales and bounds leave it out. */
+int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v,
+                  const int64_t *v_strides, int n, const int32_t *counts);
+
+/* Attention over the cache: with s = scale * <q, k_t> over the tokens that a row sees, out = sum softmax(s)_t v_t (dense
+ * [batch][n][heads_q][head_dim], the cache's type) and, where lse is not NULL, lse = log sum exp(s) (float [batch][n][heads_q]).
+ * Sums, maxima and products are float32; weights are rounded to the cache's type for their product with the values.
+ *   lists  NULL: all tokens.  Else i32 [batch][n][heads][w] (etf_kv_select's): a token sees only these blocks of the ones
+ *          that it sees as a whole (entries that are none of these are passed over; a block stands there once at
+ *          most), and the tokens up to itself of the block that it lies in
+ *   mass_out  NULL, or float [batch][heads][max_blocks] (without lists): mass_in (NULL: zeros; may be mass_out) plus the weight that
+ *          every block had in this call: the sum over the tokens' and the group's heads' rows of the softmax over its tokens,
+ *          the open block's in the entry after the full ones
+ *   ws     device, 256-byte aligned, at least etf_kv_attend_workspace_bytes (w = 0 without lists; mass != 0 with mass_out) */
+int64_t etf_kv_attend_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache, int n, int heads_q, int w, int mass);
+int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const int64_t *q_strides, int n, int heads_q, float scale,
+                  const int32_t *counts, const int32_t *lists, int w, void *out, float *lse, const float *mass_in, float *mass_out,
+                  void *ws, int64_t ws_bytes);
+
+/* Picks blocks for every (token, key/value head) from those that the token sees as a whole: the first `sink` and the last `recent`,
+ * and of the others those with the largest score, w in all (sink + recent <= w <= ETF_KV_MAX_LIST):
+ *   score = max over the group's heads of  key scale * sum_d max(q_d lo_d, q_d hi_d)
+ * with the block's bounds, which no scalar product of the block exceeds.  Decided in 64 bits, ties to the lower block.
+ * lists: i32 [batch][n][heads][w], ascending, -1 where there are fewer.  ws as above. */
+int64_t etf_kv_select_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache, int n, int heads_q, int w);
+int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const int64_t *q_strides, int n, int heads_q,
+                  const int32_t *counts, int w, int sink, int recent, int32_t *lists, void *ws, int64_t ws_bytes);
+
+/* Cuts every (sequence, head) that has more than `budget` full blocks to that many: the first `sink`, the last `recent` (sink + recent
+ * <= budget) and those of the others with the largest mass (float [batch][heads][max_blocks]; ties to the lower block, what is
+ * not a number last) stay, in their order; the open block stays too.  table_out, mass_out (entries past the full blocks: -1;
+ * the open block's weight, then 0), lens_out and evicted_out [batch] may be the arrays they are read from, or others that share
+ * nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1. */
+int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                 int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
+
 /* ---- per-kernel timing (for benchmarks) ---------------------------------- */
 
 /* Kernel classes of the hot path, in launch order. */
@@ -512,7 +598,8 @@ enum {
     ETF_K_IVF_COARSE = 11, /* IVFADC: distances to the centroids and probe selection */
     ETF_K_IVF_SCAN = 12,   /* IVFADC: scan of the probed lists                        */
     ETF_K_LDS16 = 13,      /* tree / forest candidate filter on 16-bit tables in LDS  */
-    ETF_K_COUNT = 14
+    ETF_K_KV = 14,         /* attention over a cache in 8 bits: append, attend, select, evict */
+    ETF_K_COUNT = 15
 };
 /* on != 0: every later kernel launch of this context is bracketed by a pair of
  * HIP events on the context's stream. */

@@ -28,12 +28,15 @@ EXPORTS = [
     "etf_profile_enable", "etf_profile_read", "etf_probe_bandwidth",
     "etf_ivf_set_coarse", "etf_ivf_assign_workspace_bytes", "etf_ivf_assign_device", "etf_ivf_build", "etf_ivf_stats",
     "etf_ivf_device_bytes", "etf_ivf_upload", "etf_ivf_workspace_bytes", "etf_ivf_search",
+    "etf_kv_append", "etf_kv_attend_workspace_bytes", "etf_kv_attend", "etf_kv_select_workspace_bytes", "etf_kv_select", "etf_kv_evict",
 ]
 ETF_BUILD_NONE, ETF_BUILD_CHAIN, ETF_BUILD_GENERAL, ETF_BUILD_GENERAL_AFTER_CHAIN = 0, 1, 2, 3
 ETF_PROBE_READ, ETF_PROBE_WRITE, ETF_PROBE_COPY, ETF_PROBE_ROWS, ETF_PROBE_LDS, ETF_PROBE_LDS_SCATTER = 0, 1, 2, 3, 4, 5
 ETF_PROBE_VALU_F32, ETF_PROBE_VALU_ADD3, ETF_PROBE_VALU_PK16, ETF_PROBE_MFMA_F32 = 6, 7, 8, 9
 KERNEL_CLASSES = ["lut", "level", "leaf", "flat", "reduce", "tau", "select", "exact", "sample", "lds", "encode",
-                  "ivf_coarse", "ivf_scan", "lds16"]
+                  "ivf_coarse", "ivf_scan", "lds16", "kv"]
+ETF_KV_BLOCK, ETF_KV_MAX_LIST = 64, 4096
+ETF_KV_BF16, ETF_KV_FP16 = 0, 1
 
 
 class EtfStats(ctypes.Structure):
@@ -97,6 +100,12 @@ class EtfLayout(ctypes.Structure):
         ("cb_row", ctypes.c_int32),
         ("eterm", ctypes.c_int64), ("pterm", ctypes.c_int64),
     ]
+
+
+class EtfKvCache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("pages", ctypes.c_int32)] + [
+                    (name, ctypes.c_void_p) for name in ("k", "v", "bounds", "scales", "tail_k", "tail_v", "table", "lens", "evicted")]
 
 
 class EtfError(RuntimeError):
@@ -178,6 +187,12 @@ def load_library():
         "etf_ivf_upload": (I, [P, P, L]),
         "etf_ivf_workspace_bytes": (L, [P, L, I, I]),
         "etf_ivf_search": (I, [P, P, L, I, I, P, P, P, L]),
+        "etf_kv_append": (I, [P, P, P, P, P, P, I, P]),
+        "etf_kv_attend_workspace_bytes": (L, [P, P, I, I, I, I]),
+        "etf_kv_attend": (I, [P, P, P, P, I, I, ctypes.c_float, P, P, I, P, P, P, P, P, L]),
+        "etf_kv_select_workspace_bytes": (L, [P, P, I, I, I]),
+        "etf_kv_select": (I, [P, P, P, P, I, I, P, I, I, I, P, P, L]),
+        "etf_kv_evict": (I, [P, P, P, I, I, I, P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -197,6 +212,71 @@ def _dev(t) -> int:
     return t.data_ptr()
 
 
+class KvCache:
+    """An attention cache in 8 bits: the device tensors of an etf_kv_cache, which the caller owns.
+
+    k, v, bounds: float8_e4m3fn [pages][64][D], [pages][D][64], [pages][2][D]; scales: float32 [pages][2]; tail_k, tail_v: bfloat16 or
+    float16 [B][H][2][64][D], [B][H][2][D][64]; table: int32 [B][H][max_blocks]; lens, evicted: int32 [B].
+    """
+
+    FIELDS = ("k", "v", "scales", "bounds", "tail_k", "tail_v", "table", "lens", "evicted")
+
+    def __init__(self, k, v, scales, bounds, tail_k, tail_v, table, lens, evicted):
+        import torch
+        given = dict(k=k, v=v, scales=scales, bounds=bounds, tail_k=tail_k, tail_v=tail_v, table=table, lens=lens, evicted=evicted)
+        if tail_k.dim() != 5 or table.dim() != 3 or k.dim() != 3:
+            raise ValueError("expected tail_k [B][H][2][64][D], table [B][H][max_blocks] and k [pages][64][D]")
+        B, H, _, _, D = tail_k.shape
+        pages, T = k.shape[0], tail_k.dtype
+        if T not in (torch.bfloat16, torch.float16):
+            raise ValueError("open blocks are bfloat16 or float16, not %s" % T)
+        e4m3, S = torch.float8_e4m3fn, ETF_KV_BLOCK
+        want = dict(k=((pages, S, D), e4m3), v=((pages, D, S), e4m3), scales=((pages, 2), torch.float32), bounds=((pages, 2, D), e4m3),
+                    tail_k=((B, H, 2, S, D), T), tail_v=((B, H, 2, D, S), T), table=((B, H, table.shape[2]), torch.int32),
+                    lens=((B,), torch.int32), evicted=((B,), torch.int32))
+        for name, t in given.items():
+            shape, dtype = want[name]
+            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != k.device:
+                raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (name, dtype, list(shape), k.device))
+        self._t = given
+        self.batch, self.heads, self.head_dim, self.max_blocks, self.pages, self.dtype, self.device = B, H, D, table.shape[2], pages, T, k.device
+        c = EtfKvCache(ETF_KV_BF16 if T == torch.bfloat16 else ETF_KV_FP16, B, H, D, table.shape[2], pages)
+        for name in self.FIELDS:
+            setattr(c, name, given[name].data_ptr())
+        self._c, self._ref = c, ctypes.addressof(c)
+
+    def __getattr__(self, name):
+        if name in KvCache.FIELDS:
+            return self.__dict__["_t"][name]
+        raise AttributeError(name)
+
+    @classmethod
+    def alloc(cls, batch: int, heads: int, head_dim: int, max_tokens: int, dtype=None, pages: Optional[int] = None, device="cuda"):
+        """An empty cache with room for max_tokens a sequence.  pages: None = a page for every block, already in the table;
+        else the pool's pages, the table to be filled by the caller (-1 throughout)."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        S, e4m3 = ETF_KV_BLOCK, torch.float8_e4m3fn
+        blocks = max(1, -(-max_tokens // S))
+        if pages is None:
+            pages = batch * heads * blocks
+            table = torch.arange(pages, dtype=torch.int32, device=device).view(batch, heads, blocks)
+        else:
+            table = torch.full((batch, heads, blocks), -1, dtype=torch.int32, device=device)
+        zeros = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+        return cls(zeros(pages, S, head_dim, dtype=e4m3), zeros(pages, head_dim, S, dtype=e4m3), zeros(pages, 2, dtype=torch.float32),
+                   zeros(pages, 2, head_dim, dtype=e4m3), zeros(batch, heads, 2, S, head_dim, dtype=dtype),
+                   zeros(batch, heads, 2, head_dim, S, dtype=dtype), table, zeros(batch, dtype=torch.int32), zeros(batch, dtype=torch.int32))
+
+    def fork(self) -> "KvCache":
+        """Another table, lens and evicted (uninitialised) over the same pages and open blocks, for Context.kv_evict to write."""
+        import torch
+        t = dict(self._t)
+        for name in ("table", "lens", "evicted"):
+            t[name] = torch.empty_like(t[name])
+        return KvCache(**t)
+
+
 class Context:
     """One etf_ctx.  device=None makes a host-only context (train / encode / build / stats)."""
 
@@ -207,6 +287,8 @@ class Context:
         if rc != 0:
             raise EtfError(rc, self._lib.etf_strerror(rc).decode())
         self._keep = {}     # device buffers the library refers to (index image)
+        self._stream = stream
+        self._device = None if device is None or int(device) < 0 else int(device)
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h:
@@ -228,6 +310,7 @@ class Context:
     # ---- context
     def set_stream(self, stream: Optional[int]):
         self._ck(self._lib.etf_set_stream(self._h, stream))
+        self._stream = stream
 
     def set_option(self, name: str, value: int):
         self._ck(self._lib.etf_set_option(self._h, name.encode(), int(value)))
@@ -588,6 +671,115 @@ class Context:
         p, n = self._ws(ws)
         self._ck(self._lib.etf_ivf_search(self._h, _dev(queries), Q, k, w, _dev(out_ids), _dev(out_dist), p, n))
         return out_ids, out_dist
+
+    # ---- attention over a cache in 8 bits
+    def _kv_here(self, cache: KvCache):
+        if self._device is not None and (cache.device.type, cache.device.index) != ("cuda", self._device):
+            raise ValueError("the cache is on %s, the context on GPU %d" % (cache.device, self._device))
+
+    @staticmethod
+    def _rows(t, cache: KvCache, heads: Optional[int], what: str):
+        """(pointer, strides) of rows [B][n][heads][D]; dense ones need no strides."""
+        if t.dim() != 4 or t.shape[0] != cache.batch or t.shape[3] != cache.head_dim or (heads is not None and t.shape[2] != heads) or \
+                t.dtype != cache.dtype or t.device != cache.device or t.shape[1] < 1:
+            raise ValueError("%s: expected a %s tensor [%d][n][%s][%d] on %s" % (what, cache.dtype, cache.batch, "heads" if heads is None else heads, cache.head_dim, cache.device))
+        if t.is_contiguous():
+            return t.data_ptr(), None
+        s = t.stride()
+        if s[3] != 1:
+            raise ValueError("%s: a row's elements must be contiguous" % what)
+        return t.data_ptr(), (ctypes.c_int64 * 3)(s[0], s[1], s[2])
+
+    @staticmethod
+    def _kv_dev(t, shape, dtype, cache: KvCache, what: str):
+        if t is None:
+            return None
+        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != cache.device:
+            raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (what, dtype, list(shape), cache.device))
+        return t.data_ptr()
+
+    def _kv_empty(self, shape, dtype, cache: KvCache):
+        """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
+        import torch
+        mine = self._stream or 0
+        if torch.cuda.current_stream(cache.device).cuda_stream == mine:
+            return torch.empty(shape, dtype=dtype, device=cache.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=cache.device)):
+            return torch.empty(shape, dtype=dtype, device=cache.device)
+
+    def kv_append(self, cache: KvCache, k, v, counts=None):
+        """Writes new tokens k, v [B][n][H][D] after cache.lens; the caller then advances cache.lens."""
+        import torch
+        self._kv_here(cache)
+        pk, sk = self._rows(k, cache, cache.heads, "k")
+        pv, sv = self._rows(v, cache, cache.heads, "v")
+        if v.shape[1] != k.shape[1]:
+            raise ValueError("k and v have different numbers of tokens")
+        pc = self._kv_dev(counts, (cache.batch,), torch.int32, cache, "counts")
+        self._ck(self._lib.etf_kv_append(self._h, cache._ref, pk, sk, pv, sv, k.shape[1], pc))
+
+    def kv_attend_workspace_bytes(self, cache: KvCache, n: int, heads_q: int, w: int = 0, mass: bool = False) -> int:
+        return self._ck(self._lib.etf_kv_attend_workspace_bytes(self._h, cache._ref, n, heads_q, w, int(mass)))
+
+    def kv_attend(self, cache: KvCache, q, scale: Optional[float] = None, counts=None, lists=None, out=None, lse=None, mass_in=None, mass_out=None, ws=None):
+        """Attention of q [B][n][heads_q][D] over the cache, over the blocks of lists (kv_select) if given.  scale: 1 / sqrt(D) by default."""
+        import torch
+        self._kv_here(cache)
+        pq, sq = self._rows(q, cache, None, "q")
+        B, n, heads_q, D = q.shape
+        w = 0 if lists is None else lists.shape[-1]
+        pl = self._kv_dev(lists, (B, n, cache.heads, w), torch.int32, cache, "lists")
+        pc = self._kv_dev(counts, (B,), torch.int32, cache, "counts")
+        if out is None:
+            out = self._kv_empty((B, n, heads_q, D), cache.dtype, cache)
+        po = self._kv_dev(out, (B, n, heads_q, D), cache.dtype, cache, "out")
+        pe = self._kv_dev(lse, (B, n, heads_q), torch.float32, cache, "lse")
+        blocks = (B, cache.heads, cache.max_blocks)
+        pi = self._kv_dev(mass_in, blocks, torch.float32, cache, "mass_in")
+        pm = self._kv_dev(mass_out, blocks, torch.float32, cache, "mass_out")
+        if ws is None:
+            ws = self._kv_empty((self.kv_attend_workspace_bytes(cache, n, heads_q, w, pm is not None) + 256,), torch.uint8, cache)
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_kv_attend(self._h, cache._ref, pq, sq, n, heads_q, D ** -0.5 if scale is None else scale, pc, pl, w, po, pe, pi, pm, pw, nw))
+        return out
+
+    def kv_select_workspace_bytes(self, cache: KvCache, n: int, heads_q: int, w: int) -> int:
+        return self._ck(self._lib.etf_kv_select_workspace_bytes(self._h, cache._ref, n, heads_q, w))
+
+    def kv_select(self, cache: KvCache, q, w: int, sink: int = 0, recent: int = 0, counts=None, lists=None, ws=None):
+        """Blocks for every token and key/value head: int32 [B][n][H][w], ascending, -1 where there are fewer."""
+        import torch
+        self._kv_here(cache)
+        pq, sq = self._rows(q, cache, None, "q")
+        B, n, heads_q, D = q.shape
+        pc = self._kv_dev(counts, (B,), torch.int32, cache, "counts")
+        if ws is None:
+            ws = self._kv_empty((self.kv_select_workspace_bytes(cache, n, heads_q, w) + 256,), torch.uint8, cache)
+        if lists is None:
+            lists = self._kv_empty((B, n, cache.heads, w), torch.int32, cache)
+        pl = self._kv_dev(lists, (B, n, cache.heads, w), torch.int32, cache, "lists")
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_kv_select(self._h, cache._ref, pq, sq, n, heads_q, pc, w, sink, recent, pl, pw, nw))
+        return lists
+
+    def kv_evict(self, cache: KvCache, mass, budget: int, sink: int = 0, recent: int = 0, to: Optional[KvCache] = None, mass_out=None, freed=None):
+        """Cuts every sequence's cache to `budget` full blocks by mass; returns (mass of what stays, pages taken out).  to: the
+        cache (fork()) whose table, lens and evicted are written; None: this one's, and mass is written over."""
+        import torch
+        self._kv_here(cache)
+        blocks = (cache.batch, cache.heads, cache.max_blocks)
+        pm = self._kv_dev(mass, blocks, torch.float32, cache, "mass")
+        if to is not None and (to.batch, to.heads, to.max_blocks, to.device) != (cache.batch, cache.heads, cache.max_blocks, cache.device):
+            raise ValueError("to: expected a cache with a table of the same shape on the same device")
+        if mass_out is None:
+            mass_out = mass if to is None else self._kv_empty(blocks, torch.float32, cache)
+        if freed is None:
+            freed = self._kv_empty(blocks, torch.int32, cache)
+        po = self._kv_dev(mass_out, blocks, torch.float32, cache, "mass_out")
+        pf = self._kv_dev(freed, blocks, torch.int32, cache, "freed")
+        c = (cache if to is None else to)._c
+        self._ck(self._lib.etf_kv_evict(self._h, cache._ref, pm, budget, sink, recent, c.table, c.lens, c.evicted, po, pf))
+        return mass_out, freed
 
     def probe_bandwidth(self, kind: int, a, b, nbytes: int):
         """One launch of a streaming probe kernel over the uint8 device tensors a and b (256-byte aligned)."""

@@ -1,0 +1,298 @@
+// Attention over a cache in 8 bits: checks of arguments, workspace sizes, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "etf_internal.h"
+#include "etf_launch.h"
+
+using namespace etf;
+
+namespace {
+
+#include "etf_kv_kernels.hip.h"
+
+inline int64_t al256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+constexpr int64_t GRID_MOST = 0x7FFFFFFF;
+
+// arrays: the call goes to the device and reads them
+int check_cache(const etf_ctx *ctx, const etf_kv_cache *c, bool arrays)
+{
+    if (!ctx) return ETF_EINVAL;
+    if (!c) return fail(ctx, ETF_EINVAL, "cache is null");
+    if (c->dtype != ETF_KV_BF16 && c->dtype != ETF_KV_FP16) return fail(ctx, ETF_EINVAL, "unknown cache type %d", c->dtype);
+    if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128)
+        return fail(ctx, ETF_EINVAL, "head_dim must be 64, 96 or 128 (it is %d)", c->head_dim);
+    if (c->batch < 1 || c->heads < 1 || c->max_blocks < 1 || c->pages < 1)
+        return fail(ctx, ETF_EINVAL, "batch, heads, max_blocks and pages must be positive (%d, %d, %d, %d)", c->batch, c->heads, c->max_blocks, c->pages);
+    if (c->max_blocks > (INT32_MAX >> 6) - 2 || (int64_t)c->batch * c->heads > INT32_MAX / c->max_blocks)
+        return fail(ctx, ETF_EINVAL, "batch * heads * max_blocks must stay below 2^31, tokens of a sequence too");
+    if (!arrays) return ETF_OK;
+    const void *all[] = {c->k, c->v, c->bounds, c->scales, c->tail_k, c->tail_v, c->table, c->lens, c->evicted};
+    for (const void *p : all)
+        if (!p || !aligned16(p)) return fail(ctx, ETF_EINVAL, "an array of the cache is null or not 16-byte aligned");
+    return ETF_OK;
+}
+
+// strides of sequence, token and head of rows [batch][n][heads][dim]; offsets within a sequence's rows fit the kernels' arithmetic
+int check_rows(const etf_ctx *ctx, const etf_kv_cache *c, const char *what, const void *p, const int64_t *strides, int64_t n, int64_t heads, int64_t (&out)[3])
+{
+    if (!p || !aligned16(p)) return fail(ctx, ETF_EINVAL, "%s is null or not 16-byte aligned", what);
+    if (!strides) {
+        out[2] = c->head_dim;
+        out[1] = heads * c->head_dim;
+        out[0] = n * out[1];
+        return ETF_OK;
+    }
+    for (int i = 0; i < 3; ++i) {
+        if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] > (int64_t)1 << 40)
+            return fail(ctx, ETF_EINVAL, "stride %d of %s must be a multiple of 8 elements, not negative (it is %lld)", i, what, (long long)strides[i]);
+        out[i] = strides[i];
+    }
+    return ETF_OK;
+}
+
+int check_queries(const etf_ctx *ctx, const etf_kv_cache *c, int n, int heads_q)
+{
+    if (n < 1 || heads_q < 1) return fail(ctx, ETF_EINVAL, "n and heads_q must be positive (%d, %d)", n, heads_q);
+    if (heads_q % c->heads != 0) return fail(ctx, ETF_EINVAL, "heads_q (%d) must be a multiple of the cache's heads (%d)", heads_q, c->heads);
+    if ((int64_t)n * heads_q > INT32_MAX / 16 / c->batch) return fail(ctx, ETF_EINVAL, "batch * n * heads_q must stay below 2^27");
+    return ETF_OK;
+}
+
+KvView view_of(const etf_kv_cache *c)
+{
+    return KvView{(uint8_t *)c->k, (uint8_t *)c->v, (uint8_t *)c->bounds, c->scales, (uint16_t *)c->tail_k, (uint16_t *)c->tail_v,
+                  c->table, c->lens, c->evicted, c->batch, c->heads, c->max_blocks, c->pages};
+}
+
+// calls f(type, dimensions) with the cache's as constants
+template <typename F>
+int with_shape(const etf_kv_cache *c, F f)
+{
+    auto dims = [&](auto t) {
+        switch (c->head_dim) {
+            case 64: return f(t, std::integral_constant<int, 64>());
+            case 96: return f(t, std::integral_constant<int, 96>());
+            default: return f(t, std::integral_constant<int, 128>());
+        }
+    };
+    return c->dtype == ETF_KV_BF16 ? dims(TBf()) : dims(THf());
+}
+
+int enter_device(const etf_ctx *ctx)
+{
+    if (ctx->device < 0) return fail(ctx, ETF_ENOGPU, "host-only context");
+    HIP_TRY(ctx, hipSetDevice(ctx->device));
+    return ETF_OK;
+}
+
+// How an attention call is cut up, and where its workspace's arrays lie.
+struct AttendPlan {
+    int tiles = 0, splits = 1;
+    int64_t units = 0, target = 0, grid = 0, o_ml = 0, o_row = 0, o_block = 0, total = 0;
+};
+
+AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool mass)
+{
+    AttendPlan p;
+    const int g = heads_q / c->heads;
+    const int64_t rows = (int64_t)n * g;
+    if (w > 0) {
+        p.tiles = (g + 15) / 16;
+        p.units = (int64_t)c->batch * n * c->heads * p.tiles;
+        // enough workgroups for the card, none with less than a block to a wave
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 768 / std::max<int64_t>(1, p.units)));
+        p.grid = p.units * p.splits;
+    } else {
+        p.tiles = (int)((rows + 15) / 16);
+        p.units = (int64_t)p.tiles * c->heads;
+        p.target = p.tiles > 4 ? 0 : 1024;
+        p.grid = p.target + c->batch * p.units;
+    }
+    const bool parts = w > 0 ? p.splits > 1 : p.target > 0;
+    const int64_t slots = parts ? p.grid : 0;
+    p.o_ml = al256(slots * 16 * c->head_dim * 4);
+    p.o_row = p.o_ml + al256(slots * 16 * 2 * 4);
+    const int64_t all_rows = mass ? (int64_t)c->batch * c->heads * rows : 0;
+    p.o_block = p.o_row + al256(all_rows * 4);
+    p.total = std::max<int64_t>(256, p.o_block + al256(all_rows * (c->max_blocks + 1) * 4));
+    return p;
+}
+
+template <typename T, int D, bool LIST, bool MASS>
+int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
+{
+    hipStream_t st = (hipStream_t)ctx->stream;
+    ProfScope prof(ctx, ETF_K_KV);
+    hipLaunchKernelGGL((k_kv_attend<T, D, LIST, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
+    LAUNCH_CHECK(ctx, "k_kv_attend");
+    if (LIST ? p.splits > 1 : p.target > 0) {
+        const int64_t units = LIST ? p.units : a.c.batch * p.units;
+        hipLaunchKernelGGL((k_kv_join<T, D, LIST, MASS>), dim3((unsigned)units, 16), dim3(128), 0, st, a);
+        LAUNCH_CHECK(ctx, "k_kv_join");
+    }
+    return ETF_OK;
+}
+
+}  // namespace
+
+extern "C" int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v,
+                             const int64_t *v_strides, int n, const int32_t *counts)
+{
+    int rc = check_cache(ctx, cache, true);
+    if (rc != ETF_OK) return rc;
+    if (n < 1 || n > (1 << 24)) return fail(ctx, ETF_EINVAL, "need 1 <= n <= 2^24 (n=%d)", n);
+    KvAppendArgs a{};
+    a.c = view_of(cache);
+    if ((rc = check_rows(ctx, cache, "k", k, k_strides, n, cache->heads, a.ks)) != ETF_OK) return rc;
+    if ((rc = check_rows(ctx, cache, "v", v, v_strides, n, cache->heads, a.vs)) != ETF_OK) return rc;
+    a.k = (const uint16_t *)k;
+    a.v = (const uint16_t *)v;
+    a.counts = counts;
+    a.n = n;
+    const int64_t most = std::max(1, (KB - 1 + n) / KB);  // blocks that n tokens can complete
+    a.per = (int)most;
+    const int64_t grid = (int64_t)cache->batch * cache->heads * most;
+    if (grid > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many blocks for one call");
+    if ((rc = enter_device(ctx)) != ETF_OK) return rc;
+    return with_shape(cache, [&](auto t, auto dim) {
+        ProfScope prof(ctx, ETF_K_KV);
+        hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(dim)::value>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+        LAUNCH_CHECK(ctx, "k_kv_append");
+        return (int)ETF_OK;
+    });
+}
+
+extern "C" int64_t etf_kv_attend_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache, int n, int heads_q, int w, int mass)
+{
+    int rc = check_cache(ctx, cache, false);
+    if (rc != ETF_OK) return rc;
+    if ((rc = check_queries(ctx, cache, n, heads_q)) != ETF_OK) return rc;
+    if (w < 0 || w > ETF_KV_MAX_LIST) return fail(ctx, ETF_EINVAL, "need 0 <= w <= %d (w=%d)", ETF_KV_MAX_LIST, w);
+    if (w > 0 && mass) return fail(ctx, ETF_EINVAL, "weights of blocks are not gathered over lists");
+    return plan_attend(cache, n, heads_q, w, mass != 0).total;
+}
+
+extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const int64_t *q_strides, int n, int heads_q, float scale,
+                             const int32_t *counts, const int32_t *lists, int w, void *out, float *lse, const float *mass_in, float *mass_out,
+                             void *ws, int64_t ws_bytes)
+{
+    int rc = check_cache(ctx, cache, true);
+    if (rc != ETF_OK) return rc;
+    if ((rc = check_queries(ctx, cache, n, heads_q)) != ETF_OK) return rc;
+    if (lists ? w < 1 || w > ETF_KV_MAX_LIST : w != 0) return fail(ctx, ETF_EINVAL, "need 1 <= w <= %d with lists, 0 without (w=%d)", ETF_KV_MAX_LIST, w);
+    if (lists && mass_out) return fail(ctx, ETF_EINVAL, "weights of blocks are not gathered over lists");
+    if (mass_in && !mass_out) return fail(ctx, ETF_EINVAL, "mass_in without mass_out");
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, ETF_EINVAL, "scale must be positive and finite");
+    if (!out || !aligned16(out)) return fail(ctx, ETF_EINVAL, "out is null or not 16-byte aligned");
+    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(ctx, ETF_EINVAL, "workspace is null or not 256-byte aligned");
+    const AttendPlan p = plan_attend(cache, n, heads_q, w, mass_out != nullptr);
+    if (ws_bytes < p.total) return fail(ctx, ETF_ENOMEM, "workspace too small: %lld < %lld", (long long)ws_bytes, (long long)p.total);
+    KvAttendArgs a{};
+    a.c = view_of(cache);
+    if ((rc = check_rows(ctx, cache, "q", q, q_strides, n, heads_q, a.qs)) != ETF_OK) return rc;
+    if (p.grid > GRID_MOST || (int64_t)cache->batch * p.units > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    char *base = (char *)ws;
+    a.q = (const uint16_t *)q;
+    a.counts = counts;
+    a.lists = lists;
+    a.out = (uint16_t *)out;
+    a.lse = lse;
+    a.part_o = (float *)base;
+    a.part_ml = (float *)(base + p.o_ml);
+    a.row_lse = (float *)(base + p.o_row);
+    a.block_lse = (float *)(base + p.o_block);
+    a.scale2 = scale * 1.4426950408889634f;
+    a.n = n;
+    a.g = heads_q / cache->heads;
+    a.w = w;
+    a.splits = p.splits;
+    a.tiles = p.tiles;
+    a.units = p.units;
+    a.target = p.target;
+    if ((rc = enter_device(ctx)) != ETF_OK) return rc;
+    rc = with_shape(cache, [&](auto t, auto dim) {
+        using T = decltype(t);
+        constexpr int D = decltype(dim)::value;
+        if (lists) return launch_attend<T, D, true, false>(ctx, a, p);
+        return mass_out ? launch_attend<T, D, false, true>(ctx, a, p) : launch_attend<T, D, false, false>(ctx, a, p);
+    });
+    if (rc != ETF_OK || !mass_out) return rc;
+    const int64_t grid = (int64_t)cache->batch * cache->heads * ((cache->max_blocks + 63) / 64);
+    ProfScope prof(ctx, ETF_K_KV);
+    hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, mass_in, mass_out);
+    LAUNCH_CHECK(ctx, "k_kv_mass");
+    return ETF_OK;
+}
+
+extern "C" int64_t etf_kv_select_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache, int n, int heads_q, int w)
+{
+    int rc = check_cache(ctx, cache, false);
+    if (rc != ETF_OK) return rc;
+    if ((rc = check_queries(ctx, cache, n, heads_q)) != ETF_OK) return rc;
+    if (w < 1 || w > ETF_KV_MAX_LIST) return fail(ctx, ETF_EINVAL, "need 1 <= w <= %d (w=%d)", ETF_KV_MAX_LIST, w);
+    return al256((int64_t)cache->batch * n * cache->heads * cache->max_blocks * 8);
+}
+
+extern "C" int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const int64_t *q_strides, int n, int heads_q,
+                             const int32_t *counts, int w, int sink, int recent, int32_t *lists, void *ws, int64_t ws_bytes)
+{
+    int rc = check_cache(ctx, cache, true);
+    if (rc != ETF_OK) return rc;
+    if ((rc = check_queries(ctx, cache, n, heads_q)) != ETF_OK) return rc;
+    if (w < 1 || w > ETF_KV_MAX_LIST) return fail(ctx, ETF_EINVAL, "need 1 <= w <= %d (w=%d)", ETF_KV_MAX_LIST, w);
+    if (sink < 0 || recent < 0 || sink > w || recent > w - sink) return fail(ctx, ETF_EINVAL, "need sink + recent <= w (%d, %d, %d)", sink, recent, w);
+    if (!lists) return fail(ctx, ETF_EINVAL, "lists is null");
+    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(ctx, ETF_EINVAL, "workspace is null or not 256-byte aligned");
+    const int64_t rows = (int64_t)cache->batch * n * cache->heads, need = al256(rows * cache->max_blocks * 8);
+    if (ws_bytes < need) return fail(ctx, ETF_ENOMEM, "workspace too small: %lld < %lld", (long long)ws_bytes, (long long)need);
+    KvSelectArgs a{};
+    a.c = view_of(cache);
+    if ((rc = check_rows(ctx, cache, "q", q, q_strides, n, heads_q, a.qs)) != ETF_OK) return rc;
+    const int64_t grid = rows * ((cache->max_blocks + 255) / 256);
+    if (grid > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    a.q = (const uint16_t *)q;
+    a.counts = counts;
+    a.keys = (uint64_t *)ws;
+    a.lists = lists;
+    a.n = n;
+    a.g = heads_q / cache->heads;
+    a.w = w;
+    a.sink = sink;
+    a.recent = recent;
+    if ((rc = enter_device(ctx)) != ETF_OK) return rc;
+    ProfScope prof(ctx, ETF_K_KV);
+    rc = with_shape(cache, [&](auto t, auto dim) {
+        hipLaunchKernelGGL((k_kv_score<decltype(t), decltype(dim)::value>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+        LAUNCH_CHECK(ctx, "k_kv_score");
+        return (int)ETF_OK;
+    });
+    if (rc != ETF_OK) return rc;
+    hipLaunchKernelGGL(k_kv_pick, dim3((unsigned)rows), dim3(256), 0, (hipStream_t)ctx->stream, a);
+    LAUNCH_CHECK(ctx, "k_kv_pick");
+    return ETF_OK;
+}
+
+extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                            int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed)
+{
+    int rc = check_cache(ctx, cache, true);
+    if (rc != ETF_OK) return rc;
+    if (budget < 1 || sink < 0 || recent < 0 || sink > budget || recent > budget - sink)
+        return fail(ctx, ETF_EINVAL, "need sink + recent <= budget, budget >= 1 (%d, %d, %d)", sink, recent, budget);
+    if (!mass || !table_out || !lens_out || !evicted_out || !mass_out || !freed) return fail(ctx, ETF_EINVAL, "null pointer");
+    if ((rc = enter_device(ctx)) != ETF_OK) return rc;
+    ProfScope prof(ctx, ETF_K_KV);
+    hipLaunchKernelGGL(k_kv_evict, dim3((unsigned)(cache->batch * cache->heads)), dim3(256), 0, (hipStream_t)ctx->stream, view_of(cache), mass, budget, sink,
+                       recent, table_out, mass_out, freed);
+    LAUNCH_CHECK(ctx, "k_kv_evict");
+    hipLaunchKernelGGL(k_kv_evict_lens, dim3((unsigned)((cache->batch + 63) / 64)), dim3(64), 0, (hipStream_t)ctx->stream, view_of(cache), budget, lens_out,
+                       evicted_out);
+    LAUNCH_CHECK(ctx, "k_kv_evict_lens");
+    return ETF_OK;
+}

@@ -1,0 +1,939 @@
+// Kernels of the attention cache in 8 bits (etf_kv_*): what fills it, what reads it, what picks blocks of it and what
+// thins it out.  Included by etf_kv.hip, inside its anonymous namespace.
+#pragma once
+
+constexpr int KB = 64;  // tokens of a block
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// The 16-bit type of queries, outputs and open blocks.  Codes become operands of the matrix cores exactly: four bits of
+// significand fit either type.  Keys are multiplied unscaled (their scale goes into the logits, in float32), values are
+// multiplied by a power of two on the way (`bring`).
+struct TBf {
+    typedef bf16x2 x2;
+    typedef bf16x8 x8;
+    static constexpr uint32_t EXP = 0x7F80u;  // exponent bits: all ones where a number is not finite
+    static constexpr uint16_t NOT = 0x7FC0u;
+    static __device__ __forceinline__ x2 bring(uint32_t w, float scale, bool high)
+    {
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    }
+    static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float wide(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+    static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
+    static constexpr float VHALF = 1.f;
+};
+struct THf {
+    typedef f16x2 x2;
+    typedef f16x8 x8;
+    static constexpr uint32_t EXP = 0x7C00u;
+    static constexpr uint16_t NOT = 0x7E00u;
+    static __device__ __forceinline__ x2 bring(uint32_t w, float scale, bool high)
+    {
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false);
+    }
+    static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float wide(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
+    static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
+    // a value near the type's largest may round up past it in 8 bits: values are taken at half their size
+    static constexpr float VHALF = 0.5f;
+};
+
+// eight codes (two words) as an operand
+template <typename T>
+__device__ __forceinline__ typename T::x8 bring8(uint32_t w0, uint32_t w1, float scale)
+{
+    const typename T::x2 a = T::bring(w0, scale, false), b = T::bring(w0, scale, true), c = T::bring(w1, scale, false), d = T::bring(w1, scale, true);
+    return (typename T::x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+struct KvView {
+    uint8_t *k, *v, *bounds;
+    float *scales;
+    uint16_t *tail_k, *tail_v;
+    const int32_t *table, *lens, *evicted;
+    int32_t batch, heads, blocks, pages;
+};
+
+// tokens of sequence b, within what the table has room for
+__device__ __forceinline__ int kv_len(const KvView &c, int b) { return min(max(c.lens[b], 0), c.blocks * KB + KB - 1); }
+__device__ __forceinline__ int kv_count(const int32_t *counts, int b, int n) { return counts ? min(max(counts[b], 0), n) : n; }
+// page of block j, or -1: none, or no page of the pool
+__device__ __forceinline__ int kv_page(const KvView &c, int64_t bh, int j)
+{
+    if (j < 0 || j >= c.blocks) return -1;
+    const int p = c.table[bh * c.blocks + j];
+    return p >= 0 && p < c.pages ? p : -1;
+}
+// buffer of the open block, number j
+__device__ __forceinline__ int64_t kv_tail(const KvView &c, int64_t bh, int b, int j, int D)
+{
+    return (bh * 2 + ((j + c.evicted[b]) & 1)) * (int64_t)(KB * D);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Append.  A workgroup takes one block of one (sequence, head): where the new tokens complete it, it is sealed: the
+// smallest power of two s with amax <= 448 s, codes round_e4m3(x / s) (the division is exact), the values transposed
+// through LDS so that a row of a page is one dimension's 64 tokens, and every dimension's smallest and largest key code.
+// The workgroup of the first block reads the open block's earlier tokens; it also writes what is left over into the open
+// block, afterwards, because both may be the same buffer.  A token that is not finite has keys that are not numbers
+// and values of zero: rows that see it become not a number, others do not.
+// ------------------------------------------------------------------------------------------------
+struct KvAppendArgs {
+    KvView c;
+    const uint16_t *k, *v;
+    int64_t ks[3], vs[3];  // strides of sequence, token, head
+    const int32_t *counts;
+    int n, per;  // per: workgroups of a (sequence, head), the most blocks that n tokens can complete
+};
+
+// a code's place in the order of the values
+__device__ __forceinline__ int code_order(uint32_t u)
+{
+    const int m = (int)(u & 0x7F);
+    return u & 0x80 ? -m : m;
+}
+__device__ __forceinline__ uint8_t code_of_order(int m) { return (uint8_t)(m < 0 ? 0x80 | -m : m); }
+
+template <typename T>
+__device__ __forceinline__ bool all_finite(const uint4 &w)
+{
+    constexpr uint32_t lo = T::EXP, hi = T::EXP << 16;
+    bool ok = true;
+    for (uint32_t u : {w.x, w.y, w.z, w.w}) ok = ok && (u & lo) != lo && (u & hi) != hi;
+    return ok;
+}
+
+template <typename T>
+__device__ __forceinline__ float amax8(const uint4 &w)
+{
+    float m = 0.f;
+    for (uint32_t u : {w.x, w.y, w.z, w.w}) m = fmaxf(m, fmaxf(fabsf(T::wide((uint16_t)u)), fabsf(T::wide((uint16_t)(u >> 16)))));
+    return m;
+}
+
+// eight values times 2^-e as codes
+template <typename T>
+__device__ __forceinline__ uint2 codes8(const uint4 &w, int e)
+{
+    uint32_t o[2];
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < 2; ++i) {
+        float f[4];
+        // beyond 448 only where the scale is the largest: the code of the largest value then
+        for (int j = 0; j < 4; ++j) f[j] = fminf(fmaxf(ldexpf(T::wide((uint16_t)(in[2 * i + j / 2] >> (16 * (j & 1)))), -e), -448.f), 448.f);
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+        o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], lo, true);
+    }
+    return make_uint2(o[0], o[1]);
+}
+
+// exponent of the smallest power of two s with amax <= 448 s, within what a float's normal numbers hold
+__device__ __forceinline__ int scale_exponent(float amax)
+{
+    if (!(amax > 0.f)) return 0;
+    int e;
+    const float m = frexpf(amax, &e);  // amax = m 2^e, 0.5 <= m < 1; 448 = 0.875 2^9
+    return min(max(e - (m <= 0.875f ? 9 : 8), -126), 119);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
+{
+    constexpr int PT = D / 8;                // 16-byte pieces of a token
+    constexpr int NP = KB * PT / 256;        // pieces of a thread
+    static_assert(KB * PT % 256 == 0, "pieces divide among the threads");
+    constexpr int VROW = KB + 4;             // LDS row of one dimension's value codes, padded
+    __shared__ __attribute__((aligned(16))) uint8_t s_v[D * VROW];
+    __shared__ __attribute__((aligned(16))) uint8_t s_k[KB * D];
+    __shared__ float s_amax[2][4];
+    __shared__ int s_bad[KB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t bh = blockIdx.x / a.per;
+    const int h = (int)(bh % a.c.heads), b = (int)(bh / a.c.heads), blk = blockIdx.x % a.per;
+    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
+    const int first = len / KB, begin = len % KB;
+    const int full = (begin + count) / KB, left = (begin + count) % KB;
+    if (blk > 0 && blk >= full) return;
+    const uint16_t *nk = a.k + b * a.ks[0] + h * a.ks[2], *nv = a.v + b * a.vs[0] + h * a.vs[2];
+    if (tid < KB) s_bad[tid] = 0;
+    __syncthreads();
+    if (blk < full) {
+        const int64_t old = kv_tail(a.c, bh, b, first, D);
+        uint4 kw[NP], vw[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
+            const int at = blk * KB + t - begin;  // among the new tokens
+            if (at >= 0) {
+                kw[i] = *reinterpret_cast<const uint4 *>(nk + at * a.ks[1] + d);
+                vw[i] = *reinterpret_cast<const uint4 *>(nv + at * a.vs[1] + d);
+            } else {
+                kw[i] = *reinterpret_cast<const uint4 *>(a.c.tail_k + old + t * D + d);
+                uint16_t x[8];
+                for (int j = 0; j < 8; ++j) x[j] = a.c.tail_v[old + (d + j) * KB + t];
+                vw[i] = make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+            }
+            if (!all_finite<T>(kw[i]) || !all_finite<T>(vw[i])) s_bad[t] = 1;
+        }
+        __syncthreads();
+        float mk = 0.f, mv = 0.f;
+        bool bad[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            bad[i] = s_bad[(tid + 256 * i) / PT] != 0;
+            if (!bad[i]) {
+                mk = fmaxf(mk, amax8<T>(kw[i]));
+                mv = fmaxf(mv, amax8<T>(vw[i]));
+            }
+        }
+        for (int o = 32; o; o >>= 1) {
+            mk = fmaxf(mk, __shfl_xor(mk, o));
+            mv = fmaxf(mv, __shfl_xor(mv, o));
+        }
+        if (lane == 0) {
+            s_amax[0][wave] = mk;
+            s_amax[1][wave] = mv;
+        }
+        __syncthreads();
+        const int ek = scale_exponent(fmaxf(fmaxf(s_amax[0][0], s_amax[0][1]), fmaxf(s_amax[0][2], s_amax[0][3])));
+        const int ev = scale_exponent(fmaxf(fmaxf(s_amax[1][0], s_amax[1][1]), fmaxf(s_amax[1][2], s_amax[1][3])));
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
+            uint2 ck = codes8<T>(kw[i], ek), cv = codes8<T>(vw[i], ev);
+            if (bad[i]) {
+                ck = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                cv = make_uint2(0, 0);
+            }
+            *reinterpret_cast<uint2 *>(s_k + t * D + d) = ck;
+            for (int j = 0; j < 8; ++j) s_v[(d + j) * VROW + t] = (uint8_t)((j < 4 ? cv.x : cv.y) >> (8 * (j & 3)));
+        }
+        __syncthreads();
+        const int page = kv_page(a.c, bh, first + blk);
+        if (page >= 0) {
+            for (int p = tid; p < KB * D / 16; p += 256) {
+                reinterpret_cast<uint4 *>(a.c.k + (int64_t)page * (KB * D))[p] = reinterpret_cast<const uint4 *>(s_k)[p];
+                const uint32_t *r = reinterpret_cast<const uint32_t *>(s_v + p / 4 * VROW + p % 4 * 16);
+                reinterpret_cast<uint4 *>(a.c.v + (int64_t)page * (KB * D))[p] = make_uint4(r[0], r[1], r[2], r[3]);
+            }
+            if (tid < D) {
+                int lo = 0x7F, hi = -0x7F;
+                for (int t = 0; t < KB; ++t) {
+                    if (s_bad[t]) continue;
+                    const int o = code_order(s_k[t * D + tid]);
+                    lo = min(lo, o);
+                    hi = max(hi, o);
+                }
+                if (lo > hi) lo = hi = 0;
+                a.c.bounds[((int64_t)page * 2) * D + tid] = code_of_order(lo);
+                a.c.bounds[((int64_t)page * 2 + 1) * D + tid] = code_of_order(hi);
+            }
+            if (tid < 2) a.c.scales[(int64_t)page * 2 + tid] = ldexpf(1.f, tid ? ev : ek);
+        }
+        __syncthreads();
+    }
+    if (blk > 0) return;
+    // what is left over: tokens [from, left) of the open block
+    const int from = full ? 0 : begin;
+    const int64_t now = kv_tail(a.c, bh, b, first + full, D);
+    if (first + full > a.c.blocks) return;  // no room: len stops before this
+    if (tid < KB) s_bad[tid] = 0;
+    __syncthreads();
+    const int np = (left - from) * PT;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int p = tid; p < np; p += 256) {
+            const int t = from + p / PT, d = p % PT * 8;
+            const int at = full * KB + t - begin;
+            uint4 kw = *reinterpret_cast<const uint4 *>(nk + at * a.ks[1] + d), vw = *reinterpret_cast<const uint4 *>(nv + at * a.vs[1] + d);
+            if (pass == 0) {
+                if (!all_finite<T>(kw) || !all_finite<T>(vw)) s_bad[t] = 1;
+                continue;
+            }
+            if (s_bad[t]) {
+                constexpr uint32_t two = T::NOT | (uint32_t)T::NOT << 16;
+                kw = make_uint4(two, two, two, two);
+                vw = make_uint4(0, 0, 0, 0);
+            }
+            *reinterpret_cast<uint4 *>(a.c.tail_k + now + t * D + d) = kw;
+            const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w};
+            for (int j = 0; j < 8; ++j) a.c.tail_v[now + (d + j) * KB + t] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention.  Rows are pairs (query token, query head of the group), 16 of them to a tile, which share the keys and values
+// of one key/value head.  s^T = K q^T and o^T = V^T p^T on v_mfma_f32_16x16x32: a lane's column is a row of the tile, so
+// the running maximum and sum are the lane's own and the tile of s^T is, register for register, the operand p^T of the
+// second product (which token of the block stands in which row of s^T is chosen so: row m of tile t is token
+// 16 (m / 4) + 4 t + m % 4).  Keys and values go from memory into registers, 16 bytes to a lane: the next block's keys
+// are asked for when this one's are used up, the values likewise.  A wave takes every fourth block of its workgroup's
+// range; the four join through LDS, ranges of a long cache through memory (k_kv_join).
+// ------------------------------------------------------------------------------------------------
+struct KvAttendArgs {
+    KvView c;
+    const uint16_t *q;
+    int64_t qs[3];  // strides of sequence, token, head
+    const int32_t *counts, *lists;
+    uint16_t *out;
+    float *lse;
+    float *part_o, *part_ml;  // partial results of ranges: [slot][16][D], [slot][16][2]
+    float *row_lse, *block_lse;  // logarithms (base 2) for the blocks' weights: [b][h][row], [b][h][row][blocks + 1]
+    float scale2;  // softmax scale times log2 e
+    int n, g, w, splits;
+    int tiles;        // row tiles of a (sequence, head): of all tokens, or of one token where blocks are listed
+    int64_t units;    // listed: (sequence, token, tile, head) units
+    int64_t target;   // workgroups that a whole-cache call aims at
+};
+
+constexpr int KV_LEAST = 4;  // blocks of a range, one to a wave
+
+struct KvRange {
+    int b, splits, per;  // sequence; ranges of its blocks; blocks of a range
+    int64_t first;       // number of its first workgroup
+};
+
+// Workgroup numbers of a call over whole caches: every sequence gets ranges of `per` blocks for each of its `units` (tiles of rows
+// times heads), `per` from the blocks of all sequences, so that the lengths on the device decide the split and long
+// sequences get more workgroups.  find >= 0: the sequence that workgroup `find` works for (b = batch: none); else sequence b's.
+// Every lane of the wave calls it.
+__device__ __forceinline__ KvRange kv_plan(const KvView &c, int units, int64_t target, int64_t find, int b)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int i = lane; i < c.batch; i += 64) total += (kv_len(c, i) + KB - 1) / KB;
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    KvRange r;
+    r.per = target > 0 ? (int)max((int64_t)KV_LEAST, (total * units + target - 1) / target) : 1 << 30;  // 0: no splits
+    int64_t base = 0;
+    for (int i0 = 0; i0 < c.batch; i0 += 64) {
+        const int i = i0 + lane;
+        const int s = i < c.batch ? max(1, ((kv_len(c, i) + KB - 1) / KB + r.per - 1) / r.per) : 0;
+        int64_t upto = (int64_t)s * units;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t x = __shfl_up(upto, o);
+            if (lane >= o) upto += x;
+        }
+        upto += base;
+        const uint64_t hit = __ballot(i < c.batch && (find >= 0 ? upto > find : i == b));
+        if (hit) {
+            const int l = __ffsll((unsigned long long)hit) - 1;
+            r.b = i0 + l;
+            r.splits = __builtin_amdgcn_readfirstlane(__shfl(s, l));
+            const int64_t end = __shfl(upto, l);
+            r.first = end - (int64_t)r.splits * units;
+            return r;
+        }
+        base = __shfl(upto, 63);
+    }
+    r.b = c.batch;
+    r.splits = 0;
+    r.first = 0;
+    return r;
+}
+
+__device__ __forceinline__ float row_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// A block's keys and values as they lie in a page: what one lane feeds into the products.
+template <int D>
+struct KvBlock {
+    uint4 k16[4][D / 64];
+    uint2 k8[4][1];
+    uint4 v[D / 16];
+};
+
+template <typename T, int D, bool LIST, bool MASS>
+__global__ __launch_bounds__(256) void k_kv_attend(KvAttendArgs a)
+{
+    constexpr int KS = D / 32;  // steps of the first product
+    constexpr int DT = D / 16;  // tiles of the second
+    constexpr int WIDE = D / 64, ODD = D % 64 / 32;
+    constexpr int OROW = D + 4;
+    __shared__ float s_o[4][16][OROW];
+    __shared__ float s_ml[4][16][2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 15, hq = lane >> 4;
+    const int H = a.c.heads, g = a.g;
+    int b, h, tile, token = 0, splits, from, to;
+    int64_t slot;
+    if (LIST) {
+        splits = a.splits;
+        const int64_t unit = blockIdx.x % a.units;
+        const int split = (int)(blockIdx.x / a.units);
+        slot = blockIdx.x;
+        h = (int)(unit % H);
+        tile = (int)(unit / H % a.tiles);
+        token = (int)(unit / ((int64_t)H * a.tiles) % a.n);
+        b = (int)(unit / ((int64_t)H * a.tiles * a.n));
+        const int per = (a.w + 1 + splits - 1) / splits;
+        from = split * per;
+        to = min(a.w + 1, from + per);
+    } else {
+        const int units = a.tiles * H;
+        const KvRange r = kv_plan(a.c, units, a.target, blockIdx.x, 0);
+        if (r.b >= a.c.batch) return;
+        b = r.b;
+        splits = r.splits;
+        const int local = (int)(blockIdx.x - r.first);
+        slot = blockIdx.x;
+        h = local % H;
+        tile = local / H % a.tiles;
+        from = local / units * r.per;
+        to = from + r.per;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int64_t bh = (int64_t)b * H + h;
+    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n), nb = len / KB;
+    // this lane's row, and what it sees
+    const int row = LIST ? token * g + tile * 16 + x : tile * 16 + x;
+    const int qi = LIST ? token : row / g, hg = LIST ? tile * 16 + x : row % g;
+    const bool valid = LIST ? hg < g : row < a.n * g;
+    const bool live = valid && qi < count;
+    const int sees = live ? max(0, len - count + qi + 1) : 0;
+    // what all rows of the tile see, and what any does
+    int least, most;
+    if (LIST) {
+        least = most = token < count ? max(0, len - count + token + 1) : 0;
+    } else {
+        const int i0 = tile * 16 / g, i1 = min(min(tile * 16 + 15, a.n * g - 1) / g, count - 1);
+        least = max(0, len - count + i0 + 1);
+        most = i1 >= i0 ? max(0, len - count + i1 + 1) : 0;
+        if (MASS)
+            to = min(to, (len + KB - 1) / KB);
+        else
+            to = min(to, (most + KB - 1) / KB);
+    }
+    const int whole = most / KB;  // listed: blocks that the token sees all of
+
+    typename T::x8 q[KS];
+    const uint16_t *qp = a.q + b * a.qs[0] + (valid ? qi : 0) * a.qs[1] + ((int64_t)h * g + (valid ? hg : 0)) * a.qs[2];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = *reinterpret_cast<const uint4 *>(qp + d);
+        q[ks] = __builtin_bit_cast(typename T::x8, w);
+    }
+
+    f32x4 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    // item u of the range: block j of the cache and the page it lies in (-1: none), or the open block
+    auto item = [&](int u, int &j, int &page, bool &open) {
+        open = false;
+        page = -1;
+        if (LIST) {
+            if (u == a.w) {  // the block that the token sees a part of
+                j = whole;
+                if (most % KB == 0) return;
+                open = j == nb;
+            } else {
+                j = a.lists[(((int64_t)b * a.n + token) * H + h) * a.w + u];
+                if (j < 0 || j >= whole) return;
+            }
+        } else {
+            j = u;
+            open = j == nb;
+        }
+        if (!open) page = kv_page(a.c, bh, j);
+    };
+
+    const int kt = 16 * (x / 4) + x % 4;  // this lane's token of key tile 0
+    auto load_k = [&](KvBlock<D> &r, int page) {
+        const uint8_t *p = a.c.k + (int64_t)page * (KB * D) + kt * D;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int s = 0; s < WIDE; ++s) r.k16[t][s] = *reinterpret_cast<const uint4 *>(p + 4 * t * D + 64 * s + 16 * hq);
+            if (ODD) r.k8[t][0] = *reinterpret_cast<const uint2 *>(p + 4 * t * D + 64 * WIDE + 8 * hq);
+        }
+    };
+    auto load_v = [&](KvBlock<D> &r, int page) {
+        const uint8_t *p = a.c.v + (int64_t)page * (KB * D) + x * KB + 16 * hq;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) r.v[i] = *reinterpret_cast<const uint4 *>(p + i * 16 * KB);
+    };
+
+    // logits of a block become weights: z in, p out, maximum and sum kept
+    auto softmax = [&](f32x4 (&s)[4], float scale, int j, bool all) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float z = s[t][i] * scale;
+                if (!all && j * KB + 16 * hq + 4 * t + i >= sees) z = -INFINITY;
+                s[t][i] = z;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(m, row_max(top));
+        const float base = top == -INFINITY ? 0.f : top;
+        const float fade = __builtin_amdgcn_exp2f(m - base);
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - base);
+                sum += s[t][i];
+            }
+        if (__any(top != m)) {
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] *= fade;
+        }
+        m = top;
+        l = l * fade + sum;
+        if (MASS) {
+            const float all_sum = row_sum(sum);
+            if (hq == 0 && valid) a.block_lse[(bh * a.n * g + row) * (a.c.blocks + 1) + j] = base + __builtin_amdgcn_logf(all_sum);
+        }
+    };
+    auto pack = [&](const f32x4 (&s)[4], int e) {
+        const typename T::x2 p0 = T::narrow(s[2 * e][0], s[2 * e][1]), p1 = T::narrow(s[2 * e][2], s[2 * e][3]);
+        const typename T::x2 p2 = T::narrow(s[2 * e + 1][0], s[2 * e + 1][1]), p3 = T::narrow(s[2 * e + 1][2], s[2 * e + 1][3]);
+        return (typename T::x8){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    };
+
+    KvBlock<D> r;
+    int j = 0, page = -1;
+    bool open = false;
+    int u = from + wave;
+    if (u < to) {
+        item(u, j, page, open);
+        page = __builtin_amdgcn_readfirstlane(page);
+        if (page >= 0) {
+            load_k(r, page);
+            load_v(r, page);
+        }
+    }
+    while (u < to) {
+        const int un = u + 4;
+        int jn = 0, pn = -1;
+        bool on = false;
+        if (un < to) item(un, jn, pn, on);
+        pn = __builtin_amdgcn_readfirstlane(pn);
+        f32x4 s[4];
+        if (page >= 0) {
+            const float ks = a.c.scales[(int64_t)page * 2], vs = a.c.scales[(int64_t)page * 2 + 1];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < WIDE; ++i) {
+                    s[t] = T::mfma(bring8<T>(r.k16[t][i].x, r.k16[t][i].y, 1.f), q[2 * i], s[t]);
+                    s[t] = T::mfma(bring8<T>(r.k16[t][i].z, r.k16[t][i].w, 1.f), q[2 * i + 1], s[t]);
+                }
+                if (ODD) s[t] = T::mfma(bring8<T>(r.k8[t][0].x, r.k8[t][0].y, 1.f), q[KS - 1], s[t]);
+            }
+            if (pn >= 0) load_k(r, pn);
+            softmax(s, ks * a.scale2, j, (j + 1) * KB <= least);
+            const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+            const float half = vs * T::VHALF;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                o[i] = T::mfma(bring8<T>(r.v[i].x, r.v[i].y, half), p0, o[i]);
+                o[i] = T::mfma(bring8<T>(r.v[i].z, r.v[i].w, half), p1, o[i]);
+            }
+            if (pn >= 0) load_v(r, pn);
+        } else {
+            if (open) {
+                const int64_t tail = kv_tail(a.c, bh, b, nb, D);
+                const uint16_t *tk = a.c.tail_k + tail, *tv = a.c.tail_v + tail;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
+                        s[t] = T::mfma(*reinterpret_cast<const typename T::x8 *>(tk + (kt + 4 * t) * D + d), q[ks], s[t]);
+                    }
+                }
+                softmax(s, a.scale2, j, false);
+                const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+                // what no token has written yet may be anything: its values count as zero
+                const int held = len - nb * KB - 16 * hq;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (i * 16 + x) * KB + 16 * hq + 8 * e);
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) v[y] = 8 * e + y < held ? v[y] * (decltype(v[0] + v[0]))T::VHALF : 0;
+                        o[i] = T::mfma(v, e ? p1 : p0, o[i]);
+                    }
+                }
+            } else if (MASS && j >= 0 && j <= a.c.blocks && hq == 0 && valid) {
+                a.block_lse[(bh * a.n * g + row) * (a.c.blocks + 1) + j] = -INFINITY;
+            }
+            if (pn >= 0) {
+                load_k(r, pn);
+                load_v(r, pn);
+            }
+        }
+        u = un;
+        j = jn;
+        page = pn;
+        open = on;
+    }
+
+    // the four waves' results into one
+    l = row_sum(l);
+    if (!live) {  // a row of padding: nothing seen
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    if (hq == 0) {
+        s_ml[wave][x][0] = m;
+        s_ml[wave][x][1] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4 *>(&s_o[wave][x][16 * i + 4 * hq]) = o[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * D / 4; e += 256) {
+        const int y = e / (D / 4), d = e % (D / 4) * 4;
+        const int yrow = LIST ? token * g + tile * 16 + y : tile * 16 + y;
+        const int yi = LIST ? token : yrow / g, yh = LIST ? tile * 16 + y : yrow % g;
+        if (LIST ? yh >= g : yrow >= a.n * g) continue;
+        const float top = fmaxf(fmaxf(s_ml[0][y][0], s_ml[1][y][0]), fmaxf(s_ml[2][y][0], s_ml[3][y][0]));
+        const float base = top == -INFINITY ? 0.f : top;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float all = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = __builtin_amdgcn_exp2f(s_ml[i][y][0] - base);
+            all += s_ml[i][y][1] * f;
+            sum += *reinterpret_cast<const f32x4 *>(&s_o[i][y][d]) * f;
+        }
+        if (splits > 1) {
+            *reinterpret_cast<f32x4 *>(a.part_o + (slot * 16 + y) * D + d) = sum;
+            if (d == 0) {
+                a.part_ml[(slot * 16 + y) * 2] = top;
+                a.part_ml[(slot * 16 + y) * 2 + 1] = all;
+            }
+        } else {
+            const float f = all != 0.f ? 1.f / (all * T::VHALF) : 0.f;
+            const int64_t at = ((int64_t)b * a.n + yi) * H * g + h * g + yh;
+            const typename T::x2 p0 = T::narrow(sum[0] * f, sum[1] * f), p1 = T::narrow(sum[2] * f, sum[3] * f);
+            *reinterpret_cast<uint2 *>(a.out + at * D + d) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+            if (d == 0) {
+                const float y2 = top + __builtin_amdgcn_logf(all);
+                if (a.lse) a.lse[at] = y2 * 0.69314718055994531f;
+                if (MASS) a.row_lse[bh * a.n * g + yrow] = y2;
+            }
+        }
+    }
+}
+
+// Joins the ranges of one row: a workgroup to a row of the tile, a thread to a dimension.
+template <typename T, int D, bool LIST, bool MASS>
+__global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
+{
+    const int H = a.c.heads, g = a.g, y = blockIdx.y, d = threadIdx.x;
+    int b, h, tile, token = 0, splits;
+    int64_t slot, step;
+    if (LIST) {
+        const int64_t unit = blockIdx.x;
+        h = (int)(unit % H);
+        tile = (int)(unit / H % a.tiles);
+        token = (int)(unit / ((int64_t)H * a.tiles) % a.n);
+        b = (int)(unit / ((int64_t)H * a.tiles * a.n));
+        splits = a.splits;
+        slot = unit;
+        step = a.units;
+    } else {
+        const int units = a.tiles * H;
+        h = blockIdx.x % H;
+        tile = blockIdx.x / H % a.tiles;
+        b = blockIdx.x / units;
+        const KvRange r = kv_plan(a.c, units, a.target, -1, b);
+        splits = r.splits;
+        slot = r.first + tile * H + h;
+        step = units;
+    }
+    if (splits < 2) return;
+    const int row = LIST ? token * g + tile * 16 + y : tile * 16 + y;
+    const int qi = LIST ? token : row / g, hg = LIST ? tile * 16 + y : row % g;
+    if ((LIST ? hg >= g : row >= a.n * g) || d >= D) return;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+    for (int s = 0; s < splits; ++s) {
+        const int64_t at = (slot + s * step) * 16 + y;
+        const float ms = a.part_ml[at * 2], ls = a.part_ml[at * 2 + 1], os = a.part_o[at * D + d];
+        const float top = fmaxf(m, ms), base = top == -INFINITY ? 0.f : top;
+        const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ms - base);
+        l = l * f0 + ls * f1;
+        o = o * f0 + os * f1;
+        m = top;
+    }
+    const float f = l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+    const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg;
+    const typename T::x2 p = T::narrow(o * f, 0.f);
+    a.out[at * D + d] = (uint16_t)__builtin_bit_cast(uint32_t, p);
+    if (d == 0) {
+        const float y2 = m + __builtin_amdgcn_logf(l);
+        if (a.lse) a.lse[at] = y2 * 0.69314718055994531f;
+        if (MASS) a.row_lse[((int64_t)b * H + h) * a.n * g + row] = y2;
+    }
+}
+
+// Weight of every block in this call, summed over the rows of a (sequence, head): 2^(block's logarithm - row's logarithm).
+// 64 blocks and four strands of rows to a workgroup; sums in 64 bits, in an order that does not depend on the launch.
+__global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restrict__ row_lse, const float *__restrict__ block_lse, int rows,
+                                                 const float *mass_in, float *mass_out)
+{
+    __shared__ double s_sum[4][64];
+    const int per = (c.blocks + 63) / 64;  // workgroups of a (sequence, head)
+    const int64_t bh = blockIdx.x / per;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x % per * 64 + lane;
+    const int b = (int)(bh / c.heads), held = (kv_len(c, b) + KB - 1) / KB;
+    double sum = 0;
+    if (j < min(held, c.blocks))
+        for (int r = wave; r < rows; r += 4) {
+            const float lr = row_lse[bh * rows + r];
+            if (lr == -INFINITY) continue;  // a row that sees nothing
+            sum += (double)__builtin_amdgcn_exp2f(block_lse[(bh * rows + r) * (c.blocks + 1) + j] - lr);
+        }
+    s_sum[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && j < c.blocks) {
+        sum = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+        const float was = mass_in ? mass_in[bh * c.blocks + j] : 0.f;
+        mass_out[bh * c.blocks + j] = was + (float)sum;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Selection of blocks.  score(token, head, block) = largest over the group's query heads of
+//     key scale * sum_d max(q_d lo_d, q_d hi_d),
+// which no logit of the block exceeds (before the softmax scale).  Products of a query's element and a code have at most
+// 15 bits, so sums in float64 are the same in any order unless a query's elements differ by more than 2^20 in size.
+// Scores become 64-bit keys in the same order: 0 = cannot be chosen, all ones = is always chosen.
+// ------------------------------------------------------------------------------------------------
+struct KvSelectArgs {
+    KvView c;
+    const uint16_t *q;
+    int64_t qs[3];
+    const int32_t *counts;
+    uint64_t *keys;  // [b][n][h][blocks]
+    int32_t *lists;
+    int n, g, w, sink, recent;
+};
+
+__device__ __forceinline__ uint64_t key_of(double x)
+{
+    if (x != x) return 1;  // not a number: after everything else
+    const uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);
+    return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+__device__ __forceinline__ double code_value(uint32_t u)
+{
+    const f32x2 f = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false);
+    return (double)f[0];
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
+{
+    const int H = a.c.heads;
+    const int per = (a.c.blocks + 255) / 256;  // workgroups of a (sequence, token, head)
+    const int64_t row = blockIdx.x / per;
+    const int h = (int)(row % H), i = (int)(row / H % a.n), b = (int)(row / H / a.n);
+    const int j0 = blockIdx.x % per * 256, j = j0 + threadIdx.x;
+    const int64_t bh = (int64_t)b * H + h;
+    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
+    const int whole = i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0;
+    __shared__ float s_q[D];
+    uint64_t key = 0;
+    const int page = j < whole ? kv_page(a.c, bh, j) : -1;
+    if (j0 < whole) {
+        double best = -INFINITY;
+        bool nan = false;
+        for (int hg = 0; hg < a.g; ++hg) {
+            __syncthreads();
+            if (threadIdx.x < D) s_q[threadIdx.x] = T::wide(a.q[b * a.qs[0] + i * a.qs[1] + ((int64_t)h * a.g + hg) * a.qs[2] + threadIdx.x]);
+            __syncthreads();
+            if (page < 0) continue;
+            const uint8_t *lo = a.c.bounds + (int64_t)page * (2 * D), *hi = lo + D;
+            double sum = 0;
+            for (int d = 0; d < D; d += 4) {
+                const uint32_t wl = *reinterpret_cast<const uint32_t *>(lo + d), wh = *reinterpret_cast<const uint32_t *>(hi + d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = s_q[d + e];
+                    sum += (double)x * code_value((x > 0.f ? wh : wl) >> (8 * e));
+                }
+            }
+            nan = nan || sum != sum;
+            best = fmax(best, sum);
+        }
+        if (page >= 0) key = nan ? 1 : key_of(best * (double)a.c.scales[(int64_t)page * 2]);
+        if (page >= 0 && (j < a.sink || j >= whole - a.recent)) key = ~0ull;
+    }
+    if (j < a.c.blocks) a.keys[row * a.c.blocks + j] = key;
+}
+
+// The `w` largest of `n` keys that are not zero, ties to the lower index; the workgroup of 256 calls it.  What is chosen: keys
+// above `cut`, and the first `ties` of those that equal it.
+template <typename Key>
+__device__ __forceinline__ void pick_cut(int n, int w, Key key, uint64_t &cut, int &ties)
+{
+    __shared__ int s_hist[256];
+    __shared__ uint64_t s_prefix;
+    __shared__ int s_need;
+    const int tid = threadIdx.x;
+    uint64_t prefix = 0;
+    int need = w;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        s_hist[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += 256) {
+            const uint64_t k = key(j);
+            if (k != 0 && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int left = need, d = 255;
+            while (d > 0 && s_hist[d] < left) left -= s_hist[d--];
+            s_prefix = prefix | (uint64_t)d << shift;
+            s_need = left;
+        }
+        __syncthreads();
+        prefix = s_prefix;
+        need = s_need;
+    }
+    // fewer keys than asked for: the walk ends at digit 0 everywhere, at a cut of zero, and every key lies above it
+    cut = prefix;
+    ties = need;
+}
+
+// Calls put(j, place, chosen, what load(j) gave) for every j < n, 256 of them at a time in ascending order; place = how many of
+// its kind come before it.  Everything of a round is loaded before any of it is put, and place <= j: put may write over
+// what load reads.
+template <typename Key, typename Load, typename Put>
+__device__ __forceinline__ int pick_walk(int n, uint64_t cut, int ties, Key key, Load load, Put put)
+{
+    __shared__ int s_count[2][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint64_t below = (1ull << lane) - 1;
+    int chosen = 0, equal = 0;
+    for (int j0 = 0; j0 < n; j0 += 256) {
+        const int j = j0 + tid;
+        const uint64_t k = j < n ? key(j) : 0, what = j < n ? load(j) : 0;
+        const bool over = k > cut, same = k != 0 && k == cut;
+        const uint64_t bo = __ballot(over), bs = __ballot(same);
+        __syncthreads();
+        if (lane == 0) {
+            s_count[0][wave] = __popcll(bo);
+            s_count[1][wave] = __popcll(bs);
+        }
+        __syncthreads();
+        int po = 0, ps = equal, to = 0, ts = 0;
+        for (int i = 0; i < 4; ++i) {
+            if (i < wave) {
+                po += s_count[0][i];
+                ps += s_count[1][i];
+            }
+            to += s_count[0][i];
+            ts += s_count[1][i];
+        }
+        po += __popcll(bo & below);
+        ps += __popcll(bs & below);
+        const bool take = over || (same && ps < ties);
+        // chosen ones before j: those above the cut, and of the equal ones the first `ties`
+        const int place = chosen + po + min(ps, ties) - min(equal, ties);
+        if (j < n) put(j, take ? place : j - place, take, what);
+        chosen += to + min(equal + ts, ties) - min(equal, ties);
+        equal += ts;
+    }
+    return chosen;
+}
+
+__global__ __launch_bounds__(256) void k_kv_pick(KvSelectArgs a)
+{
+    const int64_t row = blockIdx.x;  // (sequence, token, head)
+    const int H = a.c.heads, b = (int)(row / H / a.n), i = (int)(row / H % a.n);
+    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
+    const int whole = i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0;
+    const uint64_t *keys = a.keys + row * a.c.blocks;
+    int32_t *out = a.lists + row * a.w;
+    auto key = [&](int j) { return keys[j]; };
+    uint64_t cut;
+    int ties;
+    pick_cut(whole, a.w, key, cut, ties);
+    const int got = pick_walk(whole, cut, ties, key, [](int) { return (uint64_t)0; }, [&](int j, int place, bool take, uint64_t) {
+        if (take) out[place] = j;
+    });
+    for (int j = got + threadIdx.x; j < a.w; j += 256) out[j] = -1;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Eviction: of every (sequence, head) with more than `budget` blocks the first `sink`, the last `recent` and those of
+// the others with the largest weight stay, in their order.  The lengths change in a launch of their own (k_kv_evict_lens): every
+// workgroup here reads them, and they may be changed in place.
+// ------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_kv_evict(KvView c, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                                                  float *mass_out, int32_t *freed)
+{
+    const int64_t bh = blockIdx.x;
+    const int b = (int)(bh / c.heads), tid = threadIdx.x;
+    const int nb = min(kv_len(c, b) / KB, c.blocks), stay = min(nb, budget);
+    const int32_t *table = c.table + bh * c.blocks;
+    mass += bh * c.blocks;
+    table_out += bh * c.blocks;
+    mass_out += bh * c.blocks;
+    freed += bh * c.blocks;
+    const float open = nb < c.blocks ? mass[nb] : 0.f;  // the open block's weight moves along
+    auto key = [&](int j) -> uint64_t {
+        if (j < sink || j >= nb - recent) return ~0ull;
+        return key_of((double)mass[j]);
+    };
+    uint64_t cut = 0;
+    int ties = 0;
+    if (nb > budget) pick_cut(nb, budget, key, cut, ties);
+    pick_walk(
+        nb, cut, ties, key, [&](int j) { return (uint64_t)(uint32_t)table[j] << 32 | __float_as_uint(mass[j]); },
+        [&](int, int place, bool take, uint64_t what) {
+            if (take) {
+                table_out[place] = (int32_t)(what >> 32);
+                mass_out[place] = __uint_as_float((uint32_t)what);
+            } else {
+                freed[place] = (int32_t)(what >> 32);
+            }
+        });
+    __syncthreads();
+    for (int j = tid; j < c.blocks; j += 256) {
+        if (j >= stay) {
+            table_out[j] = -1;
+            mass_out[j] = j == stay && nb < c.blocks ? open : 0.f;
+        }
+        if (j >= nb - stay) freed[j] = -1;
+    }
+}
+
+__global__ __launch_bounds__(64) void k_kv_evict_lens(KvView c, int budget, int32_t *lens_out, int32_t *evicted_out)
+{
+    const int b = blockIdx.x * 64 + threadIdx.x;
+    if (b >= c.batch) return;
+    const int len = kv_len(c, b), gone = max(0, len / KB - budget);
+    lens_out[b] = len - gone * KB;
+    evicted_out[b] = c.evicted[b] + gone;
+}
