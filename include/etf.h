@@ -575,8 +575,8 @@ int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const 
 /* Cuts every (sequence, head) that has more than `budget` full blocks to that many: the first `sink`, the last `recent` (sink + recent
  * <= budget) and those of the others with the largest mass (float [batch][heads][max_blocks]; ties to the lower block, what is
  * not a number last) stay, in their order; the open block stays too.  table_out, mass_out (entries past the full blocks: -1;
- * the open block's weight, then 0), lens_out and evicted_out [batch] may be the arrays they are read from, or others that share
- * nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1. */
+ * the open block's weight, then 0), lens_out and evicted_out [batch] may be the arrays they are read from (up to
+ * 16384 blocks a row), or others that share nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1. */
 int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
                  int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
 

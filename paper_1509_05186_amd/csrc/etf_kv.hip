@@ -18,6 +18,7 @@ inline int64_t al256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 constexpr int64_t GRID_MOST = 0x7FFFFFFF;
+constexpr int KV_EVICT_MOST = 16384;  // blocks of a row that a workgroup of k_kv_evict holds
 
 // arrays: the call goes to the device and reads them
 int check_cache(const etf_ctx *ctx, const etf_kv_cache *c, bool arrays)
@@ -93,7 +94,8 @@ int enter_device(const etf_ctx *ctx)
 
 // How an attention call is cut up, and where its workspace's arrays lie.
 struct AttendPlan {
-    int tiles = 0, splits = 1;
+    bool many = false;  // tiles of 128 rows instead of 16
+    int tiles = 0, splits = 1, rows = 16;
     int64_t units = 0, target = 0, grid = 0, o_ml = 0, o_row = 0, o_block = 0, total = 0;
 };
 
@@ -109,15 +111,18 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 768 / std::max<int64_t>(1, p.units)));
         p.grid = p.units * p.splits;
     } else {
-        p.tiles = (int)((rows + 15) / 16);
+        p.many = rows > 64;
+        p.rows = p.many ? 128 : 16;
+        p.tiles = (int)((rows + p.rows - 1) / p.rows);
         p.units = (int64_t)p.tiles * c->heads;
-        p.target = p.tiles > 4 ? 0 : 1024;
+        // a card full of workgroups from the tiles alone needs no ranges
+        p.target = p.many ? (c->batch * p.units >= 1024 ? 0 : 512) : 1024;
         p.grid = p.target + c->batch * p.units;
     }
     const bool parts = w > 0 ? p.splits > 1 : p.target > 0;
-    const int64_t slots = parts ? p.grid : 0;
-    p.o_ml = al256(slots * 16 * c->head_dim * 4);
-    p.o_row = p.o_ml + al256(slots * 16 * 2 * 4);
+    const int64_t slots = parts ? p.grid * p.rows : 0;
+    p.o_ml = al256(slots * c->head_dim * 4);
+    p.o_row = p.o_ml + al256(slots * 2 * 4);
     const int64_t all_rows = mass ? (int64_t)c->batch * c->heads * rows : 0;
     p.o_block = p.o_row + al256(all_rows * 4);
     p.total = std::max<int64_t>(256, p.o_block + al256(all_rows * (c->max_blocks + 1) * 4));
@@ -129,11 +134,22 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
 {
     hipStream_t st = (hipStream_t)ctx->stream;
     ProfScope prof(ctx, ETF_K_KV);
+    if constexpr (!LIST) {
+        if (p.many) {
+            hipLaunchKernelGGL((k_kv_tile<T, D, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
+            LAUNCH_CHECK(ctx, "k_kv_tile");
+            if (p.target > 0) {
+                hipLaunchKernelGGL((k_kv_join<T, D, 128, false, MASS>), dim3((unsigned)(a.c.batch * p.units), 128), dim3(128), 0, st, a);
+                LAUNCH_CHECK(ctx, "k_kv_join");
+            }
+            return ETF_OK;
+        }
+    }
     hipLaunchKernelGGL((k_kv_attend<T, D, LIST, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_attend");
     if (LIST ? p.splits > 1 : p.target > 0) {
         const int64_t units = LIST ? p.units : a.c.batch * p.units;
-        hipLaunchKernelGGL((k_kv_join<T, D, LIST, MASS>), dim3((unsigned)units, 16), dim3(128), 0, st, a);
+        hipLaunchKernelGGL((k_kv_join<T, D, 16, LIST, MASS>), dim3((unsigned)units, 16), dim3(128), 0, st, a);
         LAUNCH_CHECK(ctx, "k_kv_join");
     }
     return ETF_OK;
@@ -223,7 +239,7 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
         return mass_out ? launch_attend<T, D, false, true>(ctx, a, p) : launch_attend<T, D, false, false>(ctx, a, p);
     });
     if (rc != ETF_OK || !mass_out) return rc;
-    const int64_t grid = (int64_t)cache->batch * cache->heads * ((cache->max_blocks + 63) / 64);
+    const int64_t grid = (int64_t)cache->batch * cache->heads * cache->max_blocks;
     ProfScope prof(ctx, ETF_K_KV);
     hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, mass_in, mass_out);
     LAUNCH_CHECK(ctx, "k_kv_mass");
@@ -254,28 +270,47 @@ extern "C" int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void
     KvSelectArgs a{};
     a.c = view_of(cache);
     if ((rc = check_rows(ctx, cache, "q", q, q_strides, n, heads_q, a.qs)) != ETF_OK) return rc;
-    const int64_t grid = rows * ((cache->max_blocks + 255) / 256);
-    if (grid > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     a.q = (const uint16_t *)q;
     a.counts = counts;
-    a.keys = (uint64_t *)ws;
+    a.scores = (uint64_t *)ws;
     a.lists = lists;
     a.n = n;
     a.g = heads_q / cache->heads;
     a.w = w;
     a.sink = sink;
     a.recent = recent;
+    a.gp = 1;
+    while (a.gp < std::min(a.g, 16)) a.gp *= 2;
+    a.tokens = 16 / a.gp;
+    a.tiles = (n + a.tokens - 1) / a.tokens;
+    const int64_t chunks = (int64_t)cache->batch * cache->heads * ((cache->max_blocks + 63) / 64);
+    // a wave keeps its blocks' bounds for several tiles of tokens, as long as there are workgroups for every compute unit
+    a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(8, chunks * a.tiles / 1024));
+    const int64_t grid = chunks * ((a.tiles + a.turns - 1) / a.turns);
+    if (grid > GRID_MOST || rows > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     ProfScope prof(ctx, ETF_K_KV);
-    rc = with_shape(cache, [&](auto t, auto dim) {
-        hipLaunchKernelGGL((k_kv_score<decltype(t), decltype(dim)::value>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+    return with_shape(cache, [&](auto t, auto dim) {
+        using T = decltype(t);
+        constexpr int D = decltype(dim)::value;
+        hipStream_t st = (hipStream_t)ctx->stream;
+        hipLaunchKernelGGL((k_kv_score<T, D>), dim3((unsigned)grid), dim3(256), 0, st, a);
         LAUNCH_CHECK(ctx, "k_kv_score");
+        // a wave to a row as long as it holds the row's keys
+        const unsigned four = (unsigned)((rows + 3) / 4), one = (unsigned)rows;
+        if (cache->max_blocks <= 256)
+            hipLaunchKernelGGL((k_kv_pick<T, D, 4, 1, 4>), dim3(four), dim3(256), 0, st, a);
+        else if (cache->max_blocks <= 1024)
+            hipLaunchKernelGGL((k_kv_pick<T, D, 4, 1, 16>), dim3(four), dim3(256), 0, st, a);
+        else if (cache->max_blocks <= 4096)
+            hipLaunchKernelGGL((k_kv_pick<T, D, 1, 4, 16>), dim3(one), dim3(256), 0, st, a);
+        else if (cache->max_blocks <= 16384)
+            hipLaunchKernelGGL((k_kv_pick<T, D, 1, 16, 16>), dim3(one), dim3(1024), 0, st, a);
+        else
+            hipLaunchKernelGGL((k_kv_pick<T, D, 1, 16, 0>), dim3(one), dim3(1024), 0, st, a);
+        LAUNCH_CHECK(ctx, "k_kv_pick");
         return (int)ETF_OK;
     });
-    if (rc != ETF_OK) return rc;
-    hipLaunchKernelGGL(k_kv_pick, dim3((unsigned)rows), dim3(256), 0, (hipStream_t)ctx->stream, a);
-    LAUNCH_CHECK(ctx, "k_kv_pick");
-    return ETF_OK;
 }
 
 extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
@@ -286,10 +321,21 @@ extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float
     if (budget < 1 || sink < 0 || recent < 0 || sink > budget || recent > budget - sink)
         return fail(ctx, ETF_EINVAL, "need sink + recent <= budget, budget >= 1 (%d, %d, %d)", sink, recent, budget);
     if (!mass || !table_out || !lens_out || !evicted_out || !mass_out || !freed) return fail(ctx, ETF_EINVAL, "null pointer");
+    if (cache->max_blocks > KV_EVICT_MOST && (table_out == cache->table || mass_out == mass))
+        return fail(ctx, ETF_EINVAL, "tables of more than %d blocks are not cut in place", KV_EVICT_MOST);
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     ProfScope prof(ctx, ETF_K_KV);
-    hipLaunchKernelGGL(k_kv_evict, dim3((unsigned)(cache->batch * cache->heads)), dim3(256), 0, (hipStream_t)ctx->stream, view_of(cache), mass, budget, sink,
-                       recent, table_out, mass_out, freed);
+    const KvView c = view_of(cache);
+    const dim3 grid((unsigned)(cache->batch * cache->heads));
+    hipStream_t st = (hipStream_t)ctx->stream;
+    if (cache->max_blocks <= 256)
+        hipLaunchKernelGGL((k_kv_evict<1, 4>), grid, dim3(64), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+    else if (cache->max_blocks <= 4096)
+        hipLaunchKernelGGL((k_kv_evict<4, 16>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+    else if (cache->max_blocks <= KV_EVICT_MOST)
+        hipLaunchKernelGGL((k_kv_evict<16, 16>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+    else
+        hipLaunchKernelGGL((k_kv_evict<16, 0>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
     LAUNCH_CHECK(ctx, "k_kv_evict");
     hipLaunchKernelGGL(k_kv_evict_lens, dim3((unsigned)((cache->batch + 63) / 64)), dim3(64), 0, (hipStream_t)ctx->stream, view_of(cache), budget, lens_out,
                        evicted_out);

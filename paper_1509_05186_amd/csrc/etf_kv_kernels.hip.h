@@ -10,6 +10,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The 16-bit type of queries, outputs and open blocks.  Codes become operands of the matrix cores exactly: four bits of
 // significand fit either type.  Keys are multiplied unscaled (their scale goes into the logits, in float32), values are
@@ -24,6 +25,7 @@ struct TBf {
         return high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
     }
     static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float wide(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
     static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
     static constexpr float VHALF = 1.f;
@@ -38,6 +40,7 @@ struct THf {
         return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false);
     }
     static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float wide(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
     static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
     // a value near the type's largest may round up past it in 8 bits: values are taken at half their size
@@ -284,8 +287,8 @@ struct KvAttendArgs {
     const int32_t *counts, *lists;
     uint16_t *out;
     float *lse;
-    float *part_o, *part_ml;  // partial results of ranges: [slot][16][D], [slot][16][2]
-    float *row_lse, *block_lse;  // logarithms (base 2) for the blocks' weights: [b][h][row], [b][h][row][blocks + 1]
+    float *part_o, *part_ml;  // partial results of ranges: [slot][rows of a tile][D], [slot][rows of a tile][2]
+    float *row_lse, *block_lse;  // logarithms (base 2) for the blocks' weights: [b][h][row], [b][h][blocks + 1][row]
     float scale2;  // softmax scale times log2 e
     int n, g, w, splits;
     int tiles;        // row tiles of a (sequence, head): of all tokens, or of one token where blocks are listed
@@ -359,7 +362,7 @@ struct KvBlock {
 };
 
 template <typename T, int D, bool LIST, bool MASS>
-__global__ __launch_bounds__(256) void k_kv_attend(KvAttendArgs a)
+__global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
 {
     constexpr int KS = D / 32;  // steps of the first product
     constexpr int DT = D / 16;  // tiles of the second
@@ -502,7 +505,7 @@ __global__ __launch_bounds__(256) void k_kv_attend(KvAttendArgs a)
         l = l * fade + sum;
         if (MASS) {
             const float all_sum = row_sum(sum);
-            if (hq == 0 && valid) a.block_lse[(bh * a.n * g + row) * (a.c.blocks + 1) + j] = base + __builtin_amdgcn_logf(all_sum);
+            if (hq == 0 && valid) a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = base + __builtin_amdgcn_logf(all_sum);
         }
     };
     auto pack = [&](const f32x4 (&s)[4], int e) {
@@ -580,7 +583,7 @@ __global__ __launch_bounds__(256) void k_kv_attend(KvAttendArgs a)
                     }
                 }
             } else if (MASS && j >= 0 && j <= a.c.blocks && hq == 0 && valid) {
-                a.block_lse[(bh * a.n * g + row) * (a.c.blocks + 1) + j] = -INFINITY;
+                a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = -INFINITY;
             }
             if (pn >= 0) {
                 load_k(r, pn);
@@ -643,8 +646,243 @@ __global__ __launch_bounds__(256) void k_kv_attend(KvAttendArgs a)
     }
 }
 
+// ------------------------------------------------------------------------------------------------
+// Attention of many rows: prompts.  128 rows to a workgroup, 32 to a wave; a block's codes are staged in LDS once for all of them
+// and become operands as they are read.  s^T = K q^T and o^T = V^T p^T on v_mfma_f32_32x32x16, again so that a lane's column is a
+// row and p^T stands in its registers as the second product wants it: row m of a tile of s^T is token
+// 16 (m / 4 % 2) + 8 (m / 16) + 4 (m / 8 % 2) + m % 4 of its 32.  The next block is on its way from memory to registers while this one
+// is worked on.  Pieces of 16 bytes are exchanged within a row of LDS, so that eight lanes that read together hit all banks.
+// ------------------------------------------------------------------------------------------------
+template <typename T, int D, bool MASS>
+__global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
+{
+    constexpr int ROWS = 128;
+    constexpr int PAIRS = D / 32;               // steps of the first product, two by two: 16 dimensions of each half of the wave
+    constexpr int DT = D / 32;                  // tiles of the second product
+    constexpr int KP = D / 16;                  // pieces of a row of keys
+    constexpr int LOADS = KB * D / 16 / 256 + (KB * D / 16 % 256 ? 1 : 0);  // pieces of a thread, of keys and of values
+    __shared__ __attribute__((aligned(16))) uint4 s_k[2][KB * D / 16], s_v[2][KB * D / 16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
+    const int H = a.c.heads, g = a.g, units = a.tiles * H;
+    const KvRange r = kv_plan(a.c, units, a.target, blockIdx.x, 0);
+    if (r.b >= a.c.batch) return;
+    const int b = __builtin_amdgcn_readfirstlane(r.b), splits = r.splits;
+    const int local = __builtin_amdgcn_readfirstlane((int)(blockIdx.x - r.first));
+    const int h = local % H, tile = a.tiles - 1 - local / H % a.tiles;  // the longest ones first
+    const int64_t bh = (int64_t)b * H + h, slot = r.first + local / units * units + tile * H + h;
+    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n), nb = len / KB;
+    auto seen_by = [&](int row) {  // what the row sees; rows past the last one like it
+        const int i = min(row, a.n * g - 1) / g;
+        return i < count ? max(0, len - count + i + 1) : 0;
+    };
+    const int row0 = tile * ROWS, wrow = row0 + 32 * wave, row = wrow + x;
+    const bool valid = row < a.n * g;
+    const int qi = min(row, a.n * g - 1) / g, hg = valid ? row % g : 0;
+    const bool live = valid && qi < count;
+    const int sees = live ? seen_by(row) : 0;
+    // the rows of one tile see no less from one to the next, up to the last one that is not padding
+    auto most_of = [&](int from, int rows) {
+        const int i0 = from / g, i1 = min(min(from + rows, a.n * g) - 1, count * g - 1) / g;
+        return from < a.n * g && i0 < count ? max(0, len - count + i1 + 1) : 0;
+    };
+    const int most = most_of(row0, ROWS), wmost = most_of(wrow, 32), wleast = wrow < a.n * g ? seen_by(wrow) : 0;
+    int from = local / units * r.per;
+    const int to = min(from + r.per, MASS ? (len + KB - 1) / KB : (most + KB - 1) / KB);
+
+    typename T::x8 q[2 * PAIRS];
+    const uint16_t *qp = a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + ((int64_t)h * g + hg) * a.qs[2];
+#pragma unroll
+    for (int i = 0; i < 2 * PAIRS; ++i) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = *reinterpret_cast<const uint4 *>(qp + 16 * (i / 2 * 2 + half) + 8 * (i % 2));
+        q[i] = __builtin_bit_cast(typename T::x8, w);
+    }
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.f);
+    float m = -INFINITY, l = 0.f;
+
+    // piece p of the keys lies at p of LDS; the piece of the row that it holds:
+    auto k_piece = [](int token, int at) { return KP == 8 ? at ^ ((token & 3) | (token >> 4 & 1) << 2) : KP == 4 ? at ^ (token & 3) : at; };
+    auto v_piece = [](int d, int at) { return at ^ (d >> 2 & 3); };
+    uint4 next_k[LOADS], next_v[LOADS];
+    auto fetch = [&](int page) {
+        const uint4 *pk = reinterpret_cast<const uint4 *>(a.c.k + (int64_t)page * (KB * D)), *pv = reinterpret_cast<const uint4 *>(a.c.v + (int64_t)page * (KB * D));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int p = tid + 256 * i;
+            if (KB * D / 16 % 256 && p >= KB * D / 16) break;
+            next_k[i] = pk[p / KP * KP + k_piece(p / KP, p % KP)];
+            next_v[i] = pv[p / 4 * 4 + v_piece(p / 4, p % 4)];
+        }
+    };
+    auto stage = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int p = tid + 256 * i;
+            if (KB * D / 16 % 256 && p >= KB * D / 16) break;
+            s_k[buf][p] = next_k[i];
+            s_v[buf][p] = next_v[i];
+        }
+    };
+    const int kt = 16 * (x >> 2 & 1) + 8 * (x >> 4) + 4 * (x >> 3 & 1) + (x & 3);  // this lane's token of tile 0
+
+    // logits of a block become weights; z = s * scale
+    auto softmax = [&](f32x16 (&s)[2], float scale, int j, bool all) {
+        if (!all) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (j * KB + 32 * t + 16 * half + i >= sees) s[t][i] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+        // the maximum in use may lag behind by a factor of 2^8 in the weights, which changes nothing but spares the scaling
+        if (__any(top > m + 8.f)) {
+            const float was = m;
+            m = fmaxf(m, top);
+            const float fade = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(was - m);
+            l *= fade;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] *= fade;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, -base));
+                sum += s[t][i];
+            }
+        l += sum;
+        if (MASS) {
+            sum += __shfl_xor(sum, 32);
+            if (half == 0 && valid) a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = base + __builtin_amdgcn_logf(sum);
+        }
+    };
+    // operand p^T of step u of tile t
+    auto pack = [&](const f32x16 &s, int u) {
+        const typename T::x2 p0 = T::narrow(s[8 * u], s[8 * u + 1]), p1 = T::narrow(s[8 * u + 2], s[8 * u + 3]);
+        const typename T::x2 p2 = T::narrow(s[8 * u + 4], s[8 * u + 5]), p3 = T::narrow(s[8 * u + 6], s[8 * u + 7]);
+        return (typename T::x8){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    };
+
+    const int paged = min(to, nb);  // the open block comes last, on its own
+    int page = from < paged ? __builtin_amdgcn_readfirstlane(kv_page(a.c, bh, from)) : -1;
+    int after = from + 1 < paged ? kv_page(a.c, bh, from + 1) : -1;
+    if (page >= 0) {
+        fetch(page);
+        stage(0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int j = from; j < paged; ++j) {
+        const int next = __builtin_amdgcn_readfirstlane(after);
+        after = j + 2 < paged ? kv_page(a.c, bh, j + 2) : -1;
+        if (next >= 0) fetch(next);
+        if (page >= 0 && (MASS || j * KB < wmost)) {
+            const float ks = a.c.scales[(int64_t)page * 2], vs = a.c.scales[(int64_t)page * 2 + 1] * T::VHALF;
+            f32x16 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = (f32x16)(0.f);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    const uint4 w = s_k[buf][(kt + 32 * t) * KP + k_piece(kt + 32 * t, 2 * i + half)];
+                    s[t] = T::mfma(bring8<T>(w.x, w.y, 1.f), q[2 * i], s[t]);
+                    s[t] = T::mfma(bring8<T>(w.z, w.w, 1.f), q[2 * i + 1], s[t]);
+                }
+            }
+            softmax(s, ks * a.scale2, j, (j + 1) * KB <= wleast);
+            typename T::x8 p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = pack(s[i / 2], i % 2);
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint4 w = s_v[buf][(32 * i + x) * 4 + v_piece(32 * i + x, 2 * t + half)];
+                    o[i] = T::mfma(bring8<T>(w.x, w.y, vs), p[2 * t], o[i]);
+                    o[i] = T::mfma(bring8<T>(w.z, w.w, vs), p[2 * t + 1], o[i]);
+                }
+        } else if (MASS && page < 0 && half == 0 && valid) {
+            a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = -INFINITY;
+        }
+        if (next >= 0) stage(buf ^ 1);
+        __syncthreads();
+        buf ^= 1;
+        page = next;
+    }
+    if (nb >= from && nb < to && (MASS || nb * KB < wmost)) {
+        const int64_t tail = kv_tail(a.c, bh, b, nb, D);
+        const uint16_t *tk = a.c.tail_k + tail, *tv = a.c.tail_v + tail;
+        f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = (f32x16)(0.f);
+#pragma unroll
+            for (int i = 0; i < 2 * PAIRS; ++i)
+                s[t] = T::mfma(*reinterpret_cast<const typename T::x8 *>(tk + (kt + 32 * t) * D + 16 * (i / 2 * 2 + half) + 8 * (i % 2)), q[i], s[t]);
+        }
+        softmax(s, a.scale2, nb, false);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const typename T::x8 p = pack(s[y / 2], y % 2);
+            // what no token has written yet may be anything: its values count as zero
+            const int at = 32 * (y / 2) + 16 * half + 8 * (y % 2), held = len - nb * KB - at;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (32 * i + x) * KB + at);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) v[z] = z < held ? v[z] * (decltype(v[0] + v[0]))T::VHALF : 0;
+                o[i] = T::mfma(v, p, o[i]);
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+    if (!live) {  // padding: nothing seen
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.f);
+    }
+    const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg, part = slot * ROWS + row - row0;
+    const float f = splits > 1 ? 1.f : l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int d = 32 * i + 8 * y + 4 * half;
+            const f32x4 v = {o[i][4 * y] * f, o[i][4 * y + 1] * f, o[i][4 * y + 2] * f, o[i][4 * y + 3] * f};
+            if (splits > 1) {
+                *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = v;
+            } else {
+                const typename T::x2 p0 = T::narrow(v[0], v[1]), p1 = T::narrow(v[2], v[3]);
+                *reinterpret_cast<uint2 *>(a.out + at * D + d) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+            }
+        }
+    if (half == 0) {
+        if (splits > 1) {
+            a.part_ml[part * 2] = m;
+            a.part_ml[part * 2 + 1] = l;
+        } else {
+            const float y2 = m + __builtin_amdgcn_logf(l);
+            if (a.lse) a.lse[at] = y2 * 0.69314718055994531f;
+            if (MASS) a.row_lse[bh * a.n * g + row] = y2;
+        }
+    }
+}
+
 // Joins the ranges of one row: a workgroup to a row of the tile, a thread to a dimension.
-template <typename T, int D, bool LIST, bool MASS>
+template <typename T, int D, int ROWS, bool LIST, bool MASS>
 __global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
 {
     const int H = a.c.heads, g = a.g, y = blockIdx.y, d = threadIdx.x;
@@ -670,12 +908,12 @@ __global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
         step = units;
     }
     if (splits < 2) return;
-    const int row = LIST ? token * g + tile * 16 + y : tile * 16 + y;
-    const int qi = LIST ? token : row / g, hg = LIST ? tile * 16 + y : row % g;
+    const int row = LIST ? token * g + tile * ROWS + y : tile * ROWS + y;
+    const int qi = LIST ? token : row / g, hg = LIST ? tile * ROWS + y : row % g;
     if ((LIST ? hg >= g : row >= a.n * g) || d >= D) return;
     float m = -INFINITY, l = 0.f, o = 0.f;
     for (int s = 0; s < splits; ++s) {
-        const int64_t at = (slot + s * step) * 16 + y;
+        const int64_t at = (slot + s * step) * ROWS + y;
         const float ms = a.part_ml[at * 2], ls = a.part_ml[at * 2 + 1], os = a.part_o[at * D + d];
         const float top = fmaxf(m, ms), base = top == -INFINITY ? 0.f : top;
         const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ms - base);
@@ -695,46 +933,49 @@ __global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
 }
 
 // Weight of every block in this call, summed over the rows of a (sequence, head): 2^(block's logarithm - row's logarithm).
-// 64 blocks and four strands of rows to a workgroup; sums in 64 bits, in an order that does not depend on the launch.
+// A workgroup to a block; sums in 64 bits, in an order that does not depend on the launch.
 __global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restrict__ row_lse, const float *__restrict__ block_lse, int rows,
                                                  const float *mass_in, float *mass_out)
 {
-    __shared__ double s_sum[4][64];
-    const int per = (c.blocks + 63) / 64;  // workgroups of a (sequence, head)
-    const int64_t bh = blockIdx.x / per;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x % per * 64 + lane;
+    __shared__ double s_sum[4];
+    const int64_t bh = blockIdx.x / c.blocks;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x % c.blocks;
     const int b = (int)(bh / c.heads), held = (kv_len(c, b) + KB - 1) / KB;
     double sum = 0;
-    if (j < min(held, c.blocks))
-        for (int r = wave; r < rows; r += 4) {
+    if (j < held)
+        for (int r = threadIdx.x; r < rows; r += 256) {
             const float lr = row_lse[bh * rows + r];
-            if (lr == -INFINITY) continue;  // a row that sees nothing
-            sum += (double)__builtin_amdgcn_exp2f(block_lse[(bh * rows + r) * (c.blocks + 1) + j] - lr);
+            // a row that sees nothing adds nothing
+            if (lr != -INFINITY) sum += (double)__builtin_amdgcn_exp2f(block_lse[(bh * (c.blocks + 1) + j) * rows + r] - lr);
         }
-    s_sum[wave][lane] = sum;
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
-    if (wave == 0 && j < c.blocks) {
-        sum = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+    if (threadIdx.x == 0) {
         const float was = mass_in ? mass_in[bh * c.blocks + j] : 0.f;
-        mass_out[bh * c.blocks + j] = was + (float)sum;
+        mass_out[bh * c.blocks + j] = was + (float)(s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
     }
 }
 
 // ------------------------------------------------------------------------------------------------
 // Selection of blocks.  score(token, head, block) = largest over the group's query heads of
-//     key scale * sum_d max(q_d lo_d, q_d hi_d),
-// which no logit of the block exceeds (before the softmax scale).  Products of a query's element and a code have at most
-// 15 bits, so sums in float64 are the same in any order unless a query's elements differ by more than 2^20 in size.
-// Scores become 64-bit keys in the same order: 0 = cannot be chosen, all ones = is always chosen.
+//     key scale * sum_d max(q_d lo_d, q_d hi_d)  =  key scale * ( <max(q, 0), hi> + <min(q, 0), lo> ),
+// which no logit of the block exceeds (before the softmax scale).  k_kv_score takes it on the matrix cores: products of a query's
+// element and a code are exact in float32, their 2 D float32 additions are off by at most 2 D 2^-24 of the terms' sizes, of which
+// no sum is larger than key scale * 448 * sum_d |q_d|.  k_kv_pick takes the choice from these scores and bounds, and evaluates
+// the blocks that they leave open in float64, where products of at most 15 bits add up to the same sum in any order
+// unless a query's elements differ by more than 2^20 in size.
 // ------------------------------------------------------------------------------------------------
 struct KvSelectArgs {
     KvView c;
     const uint16_t *q;
     int64_t qs[3];
     const int32_t *counts;
-    uint64_t *keys;  // [b][n][h][blocks]
+    uint64_t *scores;  // [b][n][h][blocks]: score and bound on its error, a float each; a bound below zero: a block that is not there
     int32_t *lists;
     int n, g, w, sink, recent;
+    int gp, tokens;  // columns of a token (its heads, the last one repeated up to a power of two), tokens of a tile of 16 columns
+    int tiles, turns;  // tiles of a sequence's tokens, tiles that a wave goes through
 };
 
 __device__ __forceinline__ uint64_t key_of(double x)
@@ -743,6 +984,11 @@ __device__ __forceinline__ uint64_t key_of(double x)
     const uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);
     return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
+__device__ __forceinline__ uint32_t key_of(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
 
 __device__ __forceinline__ double code_value(uint32_t u)
 {
@@ -750,139 +996,342 @@ __device__ __forceinline__ double code_value(uint32_t u)
     return (double)f[0];
 }
 
+__device__ __forceinline__ uint32_t positive16(uint32_t w)  // both halves: the number if its sign is plus, else 0
+{
+    const uint32_t neg = (w >> 15 & 0x00010001u) * 0xFFFFu;
+    return w & ~neg;
+}
+
+// A wave takes 16 blocks (rows of the product) and goes through tiles of 16 (token, head) columns.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
 {
-    const int H = a.c.heads;
-    const int per = (a.c.blocks + 255) / 256;  // workgroups of a (sequence, token, head)
-    const int64_t row = blockIdx.x / per;
-    const int h = (int)(row % H), i = (int)(row / H % a.n), b = (int)(row / H / a.n);
-    const int j0 = blockIdx.x % per * 256, j = j0 + threadIdx.x;
+    constexpr int KS = D / 32, WIDE = D / 64, ODD = D % 64 / 32;
+    const int H = a.c.heads, lane = threadIdx.x & 63, x = lane & 15, hq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int chunks = (a.c.blocks + 63) / 64, turns = (a.tiles + a.turns - 1) / a.turns;
+    const int h = blockIdx.x % H, turn = blockIdx.x / H % turns, chunk = blockIdx.x / H / turns % chunks, b = blockIdx.x / H / turns / chunks;
     const int64_t bh = (int64_t)b * H + h;
     const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
-    const int whole = i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0;
-    __shared__ float s_q[D];
-    uint64_t key = 0;
-    const int page = j < whole ? kv_page(a.c, bh, j) : -1;
-    if (j0 < whole) {
-        double best = -INFINITY;
-        bool nan = false;
-        for (int hg = 0; hg < a.g; ++hg) {
-            __syncthreads();
-            if (threadIdx.x < D) s_q[threadIdx.x] = T::wide(a.q[b * a.qs[0] + i * a.qs[1] + ((int64_t)h * a.g + hg) * a.qs[2] + threadIdx.x]);
-            __syncthreads();
-            if (page < 0) continue;
-            const uint8_t *lo = a.c.bounds + (int64_t)page * (2 * D), *hi = lo + D;
-            double sum = 0;
-            for (int d = 0; d < D; d += 4) {
-                const uint32_t wl = *reinterpret_cast<const uint32_t *>(lo + d), wh = *reinterpret_cast<const uint32_t *>(hi + d);
+    const int j0 = (chunk * 4 + wave) * 16;
+    const int last = min(count, (turn + 1) * a.turns * a.tokens);  // tokens from there on see no less than the others
+    if (last <= turn * a.turns * a.tokens || j0 >= min(max(0, len - count + last) / KB, a.c.blocks)) return;
+    const int page = kv_page(a.c, bh, j0 + x);
+    typename T::x8 edge[2][KS];  // lo, hi
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = s_q[d + e];
-                    sum += (double)x * code_value((x > 0.f ? wh : wl) >> (8 * e));
-                }
+    for (int e = 0; e < 2; ++e) {
+        const uint8_t *p = a.c.bounds + ((int64_t)max(page, 0) * 2 + e) * D;
+#pragma unroll
+        for (int s = 0; s < WIDE; ++s) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(p + 64 * s + 16 * hq);
+            edge[e][2 * s] = bring8<T>(w.x, w.y, 1.f);
+            edge[e][2 * s + 1] = bring8<T>(w.z, w.w, 1.f);
+        }
+        if (ODD) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(p + 64 * WIDE + 8 * hq);
+            edge[e][KS - 1] = bring8<T>(w.x, w.y, 1.f);
+        }
+    }
+    const float own = page >= 0 ? a.c.scales[(int64_t)page * 2] : -1.f;
+    float scale[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) scale[i] = __shfl(own, 4 * hq + i);
+
+    for (int tile = turn * a.turns; tile < min(a.tiles, (turn + 1) * a.turns); ++tile) {
+        const int token = tile * a.tokens + x / a.gp;
+        const bool live = x / a.gp < a.tokens && token < count;
+        f32x4 best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float size = 0.f;  // largest sum of |q_d|
+        bool odd = false;  // not a number anywhere
+        for (int g0 = 0; g0 < a.g; g0 += 16) {
+            const uint16_t *qp = a.q + b * a.qs[0] + (live ? token : 0) * a.qs[1] + ((int64_t)h * a.g + min(a.g - 1, g0 + x % a.gp)) * a.qs[2];
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+            float sum = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
+                uint4 w = make_uint4(0, 0, 0, 0);
+                if (live) w = *reinterpret_cast<const uint4 *>(qp + d);
+                uint4 p;
+                p.x = positive16(w.x);
+                p.y = positive16(w.y);
+                p.z = positive16(w.z);
+                p.w = positive16(w.w);
+                s = T::mfma(edge[1][ks], __builtin_bit_cast(typename T::x8, p), s);
+                p.x ^= w.x;
+                p.y ^= w.y;
+                p.z ^= w.z;
+                p.w ^= w.w;
+                s = T::mfma(edge[0][ks], __builtin_bit_cast(typename T::x8, p), s);
+                for (uint32_t u : {w.x, w.y, w.z, w.w}) sum += fabsf(T::wide((uint16_t)u)) + fabsf(T::wide((uint16_t)(u >> 16)));
             }
-            nan = nan || sum != sum;
-            best = fmax(best, sum);
-        }
-        if (page >= 0) key = nan ? 1 : key_of(best * (double)a.c.scales[(int64_t)page * 2]);
-        if (page >= 0 && (j < a.sink || j >= whole - a.recent)) key = ~0ull;
-    }
-    if (j < a.c.blocks) a.keys[row * a.c.blocks + j] = key;
-}
-
-// The `w` largest of `n` keys that are not zero, ties to the lower index; the workgroup of 256 calls it.  What is chosen: keys
-// above `cut`, and the first `ties` of those that equal it.
-template <typename Key>
-__device__ __forceinline__ void pick_cut(int n, int w, Key key, uint64_t &cut, int &ties)
-{
-    __shared__ int s_hist[256];
-    __shared__ uint64_t s_prefix;
-    __shared__ int s_need;
-    const int tid = threadIdx.x;
-    uint64_t prefix = 0;
-    int need = w;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        s_hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += 256) {
-            const uint64_t k = key(j);
-            if (k != 0 && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            int left = need, d = 255;
-            while (d > 0 && s_hist[d] < left) left -= s_hist[d--];
-            s_prefix = prefix | (uint64_t)d << shift;
-            s_need = left;
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        need = s_need;
-    }
-    // fewer keys than asked for: the walk ends at digit 0 everywhere, at a cut of zero, and every key lies above it
-    cut = prefix;
-    ties = need;
-}
-
-// Calls put(j, place, chosen, what load(j) gave) for every j < n, 256 of them at a time in ascending order; place = how many of
-// its kind come before it.  Everything of a round is loaded before any of it is put, and place <= j: put may write over
-// what load reads.
-template <typename Key, typename Load, typename Put>
-__device__ __forceinline__ int pick_walk(int n, uint64_t cut, int ties, Key key, Load load, Put put)
-{
-    __shared__ int s_count[2][4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint64_t below = (1ull << lane) - 1;
-    int chosen = 0, equal = 0;
-    for (int j0 = 0; j0 < n; j0 += 256) {
-        const int j = j0 + tid;
-        const uint64_t k = j < n ? key(j) : 0, what = j < n ? load(j) : 0;
-        const bool over = k > cut, same = k != 0 && k == cut;
-        const uint64_t bo = __ballot(over), bs = __ballot(same);
-        __syncthreads();
-        if (lane == 0) {
-            s_count[0][wave] = __popcll(bo);
-            s_count[1][wave] = __popcll(bs);
-        }
-        __syncthreads();
-        int po = 0, ps = equal, to = 0, ts = 0;
-        for (int i = 0; i < 4; ++i) {
-            if (i < wave) {
-                po += s_count[0][i];
-                ps += s_count[1][i];
+            size = fmaxf(size, row_sum(sum));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                odd = odd || s[i] != s[i];
+                best[i] = fmaxf(best[i], s[i]);
             }
-            to += s_count[0][i];
-            ts += s_count[1][i];
         }
-        po += __popcll(bo & below);
-        ps += __popcll(bs & below);
-        const bool take = over || (same && ps < ties);
-        // chosen ones before j: those above the cut, and of the equal ones the first `ties`
-        const int place = chosen + po + min(ps, ties) - min(equal, ties);
-        if (j < n) put(j, take ? place : j - place, take, what);
-        chosen += to + min(equal + ts, ties) - min(equal, ties);
-        equal += ts;
+        for (int o = a.gp / 2; o; o >>= 1) {
+            size = fmaxf(size, __shfl_xor(size, o));
+            odd = __shfl_xor((int)odd, o) || odd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __shfl_xor(best[i], o));
+        }
+        if (live && x % a.gp == 0) {
+            uint64_t *to = a.scores + (((int64_t)b * a.n + token) * H + h) * a.c.blocks + j0 + 4 * hq;
+            // twice what the additions can be off by: the bound's own arithmetic, and the sums of score and bound, are rounded too
+            const float off = (4 * D + 16) * 5.9604645e-8f * 448.f * size;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float2 v = make_float2(best[i] * scale[i], off * scale[i]);
+                if (scale[i] < 0.f)
+                    v = make_float2(0.f, -1.f);
+                else if (odd || !(fabsf(v.x) < INFINITY) || !(v.y < INFINITY))
+                    v = make_float2(0.f, INFINITY);  // whatever it is: k_kv_pick looks
+                if (j0 + 4 * hq + i < a.c.blocks) to[i] = (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x);
+            }
+        }
     }
-    return chosen;
 }
 
-__global__ __launch_bounds__(256) void k_kv_pick(KvSelectArgs a)
+// ------------------------------------------------------------------------------------------------
+// The `w` largest of `n` keys that are not zero, ties to the lower index.  WAVES waves take one row together; a wave holds up to 64 KPT
+// consecutive keys in registers.  The w-th largest key is found bit by bit from the top: a candidate is kept if at least w
+// keys reach it, counted by ballots, and the walk ends early once exactly w do, which keys of scores decide after some twenty
+// bits.  Rows longer than the registers read their keys again for every bit (KPT = 0).
+// ------------------------------------------------------------------------------------------------
+template <typename U, int WAVES, int KPT>
+struct Pick {
+    static constexpr int KEYS = KPT ? KPT : 1;
+    U keys[KEYS];
+    U cut = 0;  // chosen: keys above it, and the first `ties` of those that equal it
+    int ties = 0;
+    int n, from;       // keys of the row; first of this wave's
+    int span;          // keys of a wave, a multiple of 64
+
+    static __device__ __forceinline__ int wave() { return WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
+
+    template <typename Key>
+    __device__ __forceinline__ U at(int i, Key key) const
+    {
+        if (KPT) return keys[i];
+        const int j = from + 64 * i + lane();
+        return j < n ? key(j) : 0;
+    }
+
+    // keys that reach x, over all waves
+    template <typename Key>
+    __device__ __forceinline__ int reach(U x, Key key, int (&s_sum)[2][WAVES], int turn) const
+    {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            if (KPT && from + 64 * i >= n) break;
+            if (KPT) {
+                c += __popcll(__ballot(keys[i] >= x));
+            } else {
+                for (int k = 0; k < span && from + k < n; k += 64) c += __popcll(__ballot(at(k / 64, key) >= x));
+            }
+        }
+        if (WAVES == 1) return c;
+        if (lane() == 0) s_sum[turn][wave()] = c;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all += s_sum[turn][i];
+        return all;
+    }
+
+    template <typename Key>
+    __device__ __forceinline__ void load(int n_, Key key)
+    {
+        n = n_;
+        span = KPT ? 64 * KPT : (n + 64 * WAVES - 1) / (64 * WAVES) * 64;
+        from = wave() * span;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int j = from + 64 * i + lane();
+            keys[i] = KPT && j < n ? key(j) : 0;
+        }
+    }
+
+    // after load(); turn: the buffer of the row's last count
+    template <typename Key>
+    __device__ __forceinline__ void find(int w, Key key, int (&s_sum)[2][WAVES], int &turn)
+    {
+        const int have = reach(1, key, s_sum, turn ^= 1);
+        if (have <= w) return;  // no more than asked for: all of them
+        U x = 0;
+        for (int bit = 8 * (int)sizeof(U) - 1; bit >= 0; --bit) {
+            const U y = x | (U)1 << bit;
+            const int c = reach(y, key, s_sum, turn ^= 1);
+            if (c == w) {
+                cut = y - 1;
+                return;
+            }
+            if (c > w) x = y;
+        }
+        // x is the w-th largest key, and more than one equals it
+        cut = x;
+        ties = w - (x == (U)~(U)0 ? 0 : reach(x + 1, key, s_sum, turn ^= 1));
+    }
+
+    // Calls put(j, place, chosen) for every j < n, place = how many of its kind come before it; returns the number of chosen ones.
+    template <typename Key, typename Put>
+    __device__ __forceinline__ int walk(Key key, Put put) const
+    {
+        __shared__ int s_kind[2][WAVES];
+        int over = 0, same = 0, all = 0;
+        if (WAVES > 1) {
+            for (int k = 0; k < span && from + k < n; k += 64) {
+                const U v = at(k / 64, key);
+                over += __popcll(__ballot(v > cut));
+                same += __popcll(__ballot(v != 0 && v == cut));
+            }
+            if (lane() == 0) {
+                s_kind[0][wave()] = over;
+                s_kind[1][wave()] = same;
+            }
+            __syncthreads();
+            over = same = 0;
+            for (int i = 0; i < wave(); ++i) {
+                over += s_kind[0][i];
+                same += s_kind[1][i];
+            }
+            int so = 0, ss = 0;
+            for (int i = 0; i < WAVES; ++i) {
+                so += s_kind[0][i];
+                ss += s_kind[1][i];
+            }
+            all = so + min(ss, ties);
+        }
+        const uint64_t below = (1ull << lane()) - 1;
+#pragma unroll
+        for (int i = 0; i < (KPT ? KPT : 1); ++i) {
+            for (int k = KPT ? 64 * i : 0; k < (KPT ? 64 * i + 1 : span) && from + k < n; k += 64) {
+                const int j = from + k + lane();
+                const U v = KPT ? keys[i] : at(k / 64, key);
+                const uint64_t bo = __ballot(v > cut), bs = __ballot(v != 0 && v == cut);
+                const int os = same + __popcll(bs & below);
+                const bool take = v > cut || (v != 0 && v == cut && os < ties);
+                const int place = over + __popcll(bo & below) + min(os, ties);
+                if (j < n) put(j, take ? place : j - place, take);
+                over += __popcll(bo);
+                same += __popcll(bs);
+            }
+        }
+        return WAVES == 1 ? over + min(same, ties) : all;
+    }
+};
+
+// The score of one block in float64, by 16 lanes together: lane `part` of them has every 16th dimension.
+template <typename T>
+__device__ __forceinline__ double exact_score(const KvSelectArgs &a, const uint16_t *q, int page, int D, int part)
 {
-    const int64_t row = blockIdx.x;  // (sequence, token, head)
-    const int H = a.c.heads, b = (int)(row / H / a.n), i = (int)(row / H % a.n);
+    const uint8_t *lo = a.c.bounds + (int64_t)page * (2 * D), *hi = lo + D;
+    double best = -INFINITY;
+    bool odd = false;
+    for (int hg = 0; hg < a.g; ++hg) {
+        double sum = 0;
+        for (int d = part; d < D; d += 16) {
+            const float x = T::wide(q[hg * a.qs[2] + d]);
+            sum += (double)x * code_value(x > 0.f ? hi[d] : lo[d]);
+        }
+        for (int o = 8; o; o >>= 1) sum += __shfl_xor(sum, o);
+        odd = odd || sum != sum;
+        best = fmax(best, sum);
+    }
+    return odd ? NAN : best * (double)a.c.scales[(int64_t)page * 2];
+}
+
+// ROWS rows to a workgroup, WAVES waves to a row (one of the two is 1).  From the scores' intervals: no block below the w-th largest
+// lower end can be chosen, and any whose lower end lies above the (w + 1)-th largest upper end is; the rest are
+// evaluated, as a rule none or two.
+template <typename T, int D, int ROWS, int WAVES, int KPT>
+__global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
+{
+    const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);  // (sequence, token, head)
+    const int H = a.c.heads, b = (int)(row / H / a.n), i = (int)(row / H % a.n), h = (int)(row % H);
+    if (b >= a.c.batch) return;
     const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
     const int whole = i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0;
-    const uint64_t *keys = a.keys + row * a.c.blocks;
+    __shared__ int s_sum[2][WAVES];
+    int turn = 0;
+    uint64_t *scores = a.scores + row * a.c.blocks;
     int32_t *out = a.lists + row * a.w;
-    auto key = [&](int j) { return keys[j]; };
-    uint64_t cut;
-    int ties;
-    pick_cut(whole, a.w, key, cut, ties);
-    const int got = pick_walk(whole, cut, ties, key, [](int) { return (uint64_t)0; }, [&](int j, int place, bool take, uint64_t) {
+    auto at = [&](int j, float &v, float &off) {
+        const uint64_t u = scores[j];
+        v = __uint_as_float((uint32_t)u);
+        off = __uint_as_float((uint32_t)(u >> 32));
+    };
+    auto forced = [&](int j) { return j < a.sink || j >= whole - a.recent; };
+    auto low = [&](int j) -> uint32_t {
+        float v, off;
+        at(j, v, off);
+        if (off < 0.f) return 0;
+        return forced(j) ? ~0u : off == INFINITY ? 1 : key_of(v - off);
+    };
+    auto high = [&](int j) -> uint32_t {
+        float v, off;
+        at(j, v, off);
+        if (off < 0.f) return 0;
+        return forced(j) ? ~0u : off == INFINITY ? ~0u - 1 : key_of(v + off);
+    };
+    auto put = [&](int j, int place, bool take) {
         if (take) out[place] = j;
-    });
-    for (int j = got + threadIdx.x; j < a.w; j += 256) out[j] = -1;
+    };
+    int got;
+    Pick<uint32_t, WAVES, KPT> lower, upper;
+    lower.load(whole, low);
+    lower.find(a.w, low, s_sum, turn);
+    // w blocks reach `least` with their lower ends: one whose upper end does not cannot be chosen
+    const uint32_t least = lower.ties ? lower.cut : lower.cut + 1;
+    upper.load(whole, high);
+    if (upper.reach(least, high, s_sum, turn ^= 1) <= a.w) {
+        upper.cut = least - 1;
+        got = upper.walk(high, put);
+    } else {
+        // no more than w upper ends lie above `sure`: a block whose lower end does is chosen
+        upper.find(a.w, high, s_sum, turn);
+        const uint32_t sure = upper.cut;
+        const int lane = threadIdx.x & 63;
+        const uint16_t *q = a.q + b * a.qs[0] + i * a.qs[1] + (int64_t)h * a.g * a.qs[2];
+        for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
+            const int j = lower.from + k + lane;
+            const bool here = j < whole;
+            float v = 0.f, off = -1.f;
+            if (here) at(j, v, off);
+            const uint32_t lo = here ? low(j) : 0, hi = here ? high(j) : 0;
+            uint64_t key = hi < least ? 0 : lo > sure || lo == ~0u ? ~0ull : 2;
+            if (key == 2 && off == 0.f) key = key_of((double)v);  // a query of zeros
+            uint64_t open = __ballot(key == 2);
+            while (open) {  // four blocks at a time, 16 lanes to each
+                int bit[4], mine = -1;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    bit[y] = __ffsll((unsigned long long)open) - 1;  // -1: none left
+                    if (lane / 16 == y) mine = bit[y];
+                    open &= open - 1;
+                }
+                const int page = mine >= 0 ? kv_page(a.c, (int64_t)b * H + h, lower.from + k + mine) : 0;
+                const double score = exact_score<T>(a, q, max(page, 0), D, lane & 15);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const double one = __shfl(score, 16 * y);
+                    if (lane == bit[y]) key = key_of(one);
+                }
+            }
+            if (here) scores[j] = key;  // a block's key takes its score's place
+        }
+        auto key = [&](int j) { return scores[j]; };
+        Pick<uint64_t, WAVES, KPT> last;
+        last.load(whole, key);
+        last.find(a.w, key, s_sum, turn);
+        got = last.walk(key, put);
+    }
+    for (int j = got + threadIdx.x % (64 * WAVES); j < a.w; j += 64 * WAVES) out[j] = -1;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -890,8 +1339,11 @@ __global__ __launch_bounds__(256) void k_kv_pick(KvSelectArgs a)
 // the others with the largest weight stay, in their order.  The lengths change in a launch of their own (k_kv_evict_lens): every
 // workgroup here reads them, and they may be changed in place.
 // ------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void k_kv_evict(KvView c, const float *mass, int budget, int sink, int recent, int32_t *table_out,
-                                                  float *mass_out, int32_t *freed)
+// Everything is read before anything is written, since the outputs may be the inputs; with more blocks than the registers hold a launch
+// of one workgroup per row has to write apart from what it reads (KPT = 0: `table_out` and `mass_out` are not the inputs).
+template <int WAVES, int KPT>
+__global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *mass, int budget, int sink, int recent, int32_t *table_out, float *mass_out,
+                                                         int32_t *freed)
 {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / c.heads), tid = threadIdx.x;
@@ -906,21 +1358,49 @@ __global__ __launch_bounds__(256) void k_kv_evict(KvView c, const float *mass, i
         if (j < sink || j >= nb - recent) return ~0ull;
         return key_of((double)mass[j]);
     };
-    uint64_t cut = 0;
-    int ties = 0;
-    if (nb > budget) pick_cut(nb, budget, key, cut, ties);
-    pick_walk(
-        nb, cut, ties, key, [&](int j) { return (uint64_t)(uint32_t)table[j] << 32 | __float_as_uint(mass[j]); },
-        [&](int, int place, bool take, uint64_t what) {
-            if (take) {
-                table_out[place] = (int32_t)(what >> 32);
-                mass_out[place] = __uint_as_float((uint32_t)what);
-            } else {
-                freed[place] = (int32_t)(what >> 32);
+    __shared__ int s_sum[2][WAVES];
+    int turn = 0;
+    Pick<uint64_t, WAVES, KPT> pick;
+    pick.load(nb, key);
+    pick.find(budget, key, s_sum, turn);
+    int32_t page[KPT ? KPT : 1];
+    float weight[KPT ? KPT : 1];
+    if (KPT) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int j = pick.from + 64 * i + pick.lane();
+            if (j < nb) {
+                page[i] = table[j];
+                weight[i] = mass[j];
             }
-        });
+        }
+        __syncthreads();
+    }
+    pick.walk(key, [&](int j, int place, bool take) {
+        int32_t p;
+        float w;
+        if (KPT) {
+            p = 0;
+            w = 0.f;
+#pragma unroll
+            for (int i = 0; i < KPT; ++i)
+                if (j - pick.lane() - pick.from == 64 * i) {
+                    p = page[i];
+                    w = weight[i];
+                }
+        } else {
+            p = table[j];
+            w = mass[j];
+        }
+        if (take) {
+            table_out[place] = p;
+            mass_out[place] = w;
+        } else {
+            freed[place] = p;
+        }
+    });
     __syncthreads();
-    for (int j = tid; j < c.blocks; j += 256) {
+    for (int j = tid; j < c.blocks; j += 64 * WAVES) {
         if (j >= stay) {
             table_out[j] = -1;
             mass_out[j] = j == stay && nb < c.blocks ? open : 0.f;

@@ -407,6 +407,48 @@ def test_select_decides_what_float32_cannot():
         assert torch.equal(lists.cpu(), kv.select(c, q, w, 0, 0))
 
 
+def bounds_only(D, blocks, whole, distinct, seed, H=1, dtype=BF):
+    """A cache whose blocks have bounds and scales (distinct ones, then the same again) and no content."""
+    g = torch.Generator().manual_seed(seed)
+    table = torch.randint(0, distinct, (1, H, blocks), generator=g) if distinct < whole else torch.randperm(distinct, generator=g)[:blocks].expand(1, H, -1).clone()
+    c = kv.new_cache(1, H, D, blocks, dtype, pages=distinct, table=table)
+    edges = torch.sort(torch.randn(distinct, 2, D, generator=g) * 100, dim=1)[0].clamp(-448, 448)
+    c["bounds"].copy_(edges.to(torch.float8_e4m3fn))
+    c["scales"].copy_(torch.exp2(torch.randint(-6, -3, (distinct, 2), generator=g).float()))
+    c["lens"][0] = 64 * whole + 7
+    return c, g
+
+
+@pytest.mark.parametrize("blocks,whole,distinct,w", [(300, 256, 300, 9), (1100, 1030, 1100, 40), (1100, 1090, 30, 100), (4200, 4100, 4200, 64), (4200, 4097, 5, 1000),
+                                                     (17000, 16500, 17000, 100), (17000, 2100, 17000, 3000), (17000, 16390, 60, 300)])
+def test_select_from_long_tables(blocks, whole, distinct, w):
+    say("long tables", blocks, whole, distinct, w)
+    c, g = bounds_only(64, blocks, whole, distinct, 70 + w)
+    c["table"][0, 0, 11], c["table"][0, 0, whole - 3] = -1, distinct
+    q = queries(g, BF, 1, 2, 3, 64)
+    lists = context().kv_select(on_gpu(c), q.cuda(), w, sink=2, recent=1)
+    assert torch.equal(lists.cpu(), kv.select(c, q, w, 2, 1))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_select_scores_that_float32_does_not_hold(dtype):
+    """Scores past float32's largest, queries that are not finite, a block among many with a scale far above the others'."""
+    say("far scores", dtype)
+    c, g = bounds_only(96, 300, 290, 300, 80, dtype=dtype)
+    q = queries(g, dtype, 1, 4, 2, 96)
+    if dtype == BF:
+        c["scales"][:, 0] *= 2.0 ** 100
+        q[0, 0] *= 2.0 ** 30
+        q[0, 1] *= 2.0 ** 100
+    c["scales"][int(c["table"][0, 0, 100]), 0] *= 2.0 ** 14
+    q[0, 2, 1] = 0
+    want = kv.select(c, q, 12, 1, 1)
+    assert torch.equal(context().kv_select(on_gpu(c), q.cuda(), 12, sink=1, recent=1).cpu(), want)
+    q[0, 3, 0, 5] = math.nan                    # every score is not a number: all equal, and the others' rows stay
+    got = context().kv_select(on_gpu(c), q.cuda(), 12, sink=1, recent=1).cpu()
+    assert torch.equal(got[:, :3], want[:, :3]) and got[0, 3, 0].tolist() == list(range(11)) + [289]
+
+
 def test_lists_that_name_no_block_that_is_seen():
     say("odd lists")
     c, rand = filled(HF, 128, 2, [200, 64], seed=32)
@@ -447,6 +489,30 @@ def test_evict(blocks, lens, budget, sink, recent):
     kept, freed = ctx.kv_evict(cache, own, budget, sink=sink, recent=recent)
     for x, y in zip((cache.table, cache.lens, cache.evicted, own, freed), want):
         assert torch.equal(torch.nan_to_num(x.cpu(), nan=-9.0), torch.nan_to_num(y, nan=-9.0))
+
+
+def test_evict_from_long_tables():
+    say("long tables")
+    for blocks, n in ((1100, 1050), (5000, 4500), (17000, 16400)):
+        g = torch.Generator().manual_seed(blocks)
+        c = kv.new_cache(1, 2, 64, blocks, BF, pages=8, table=torch.randint(0, 8, (1, 2, blocks), generator=g))
+        c["lens"][0] = 64 * n + 1
+        mass = torch.randint(0, 500, (1, 2, blocks), generator=g).float()
+        want = kv.evict(c, mass, 700, 3, 20)
+        cache, ctx = on_gpu(c), context()
+        to = cache.fork()
+        kept, freed = ctx.kv_evict(cache, mass.cuda(), 700, sink=3, recent=20, to=to)
+        for x, y in zip((to.table, to.lens, to.evicted, kept, freed), want):
+            assert torch.equal(x.cpu(), y)
+        if blocks <= 16384:
+            own = mass.cuda()
+            kept, freed = ctx.kv_evict(cache, own, 700, sink=3, recent=20)
+            for x, y in zip((cache.table, cache.lens, cache.evicted, own, freed), want):
+                assert torch.equal(x.cpu(), y)
+        else:
+            with pytest.raises(etf.EtfError) as e:
+                ctx.kv_evict(cache, mass.cuda(), 700)
+            assert e.value.code == -1
 
 
 def test_a_cache_that_is_cut_goes_on():

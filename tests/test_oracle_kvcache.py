@@ -183,6 +183,11 @@ def test_arguments_that_are_refused(host):
     for bad in (dict(mass=None), dict(budget=0), dict(sink=-1), dict(recent=-2), dict(sink=3, recent=2), dict(table=None), dict(lens=None), dict(evicted=None),
                 dict(out=None), dict(freed=None)):
         assert evict(**bad) == -1, bad
+    c.max_blocks = 16385                                    # too long a row to be cut in place
+    assert evict() == -1 and evict(table=8192) == -1 and evict(table=8192, out=8192) == -5
+    c.max_blocks = 16384
+    assert evict() == -5
+    c.max_blocks = 8
 
 
 def test_the_bindings_checks():
