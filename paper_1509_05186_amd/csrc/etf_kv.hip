@@ -139,7 +139,7 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
             hipLaunchKernelGGL((k_kv_tile<T, D, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
             LAUNCH_CHECK(ctx, "k_kv_tile");
             if (p.target > 0) {
-                hipLaunchKernelGGL((k_kv_join<T, D, 128, false, MASS>), dim3((unsigned)(a.c.batch * p.units), 128), dim3(128), 0, st, a);
+                hipLaunchKernelGGL((k_kv_join<T, D, 128, false, MASS>), dim3((unsigned)(a.c.batch * p.units * 16)), dim3(256), 0, st, a);
                 LAUNCH_CHECK(ctx, "k_kv_join");
             }
             return ETF_OK;
@@ -149,7 +149,7 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
     LAUNCH_CHECK(ctx, "k_kv_attend");
     if (LIST ? p.splits > 1 : p.target > 0) {
         const int64_t units = LIST ? p.units : a.c.batch * p.units;
-        hipLaunchKernelGGL((k_kv_join<T, D, 16, LIST, MASS>), dim3((unsigned)units, 16), dim3(128), 0, st, a);
+        hipLaunchKernelGGL((k_kv_join<T, D, 16, LIST, MASS>), dim3((unsigned)units * 2), dim3(256), 0, st, a);
         LAUNCH_CHECK(ctx, "k_kv_join");
     }
     return ETF_OK;
@@ -212,7 +212,7 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
     KvAttendArgs a{};
     a.c = view_of(cache);
     if ((rc = check_rows(ctx, cache, "q", q, q_strides, n, heads_q, a.qs)) != ETF_OK) return rc;
-    if (p.grid > GRID_MOST || (int64_t)cache->batch * p.units > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    if (p.grid > GRID_MOST || (lists ? 2 * p.units : cache->batch * p.units * (p.rows / 8)) > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     char *base = (char *)ws;
     a.q = (const uint16_t *)q;
     a.counts = counts;

@@ -8,6 +8,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -359,6 +360,7 @@ struct KvBlock {
     uint4 k16[4][D / 64];
     uint2 k8[4][1];
     uint4 v[D / 16];
+    f32x2 scales;
 };
 
 template <typename T, int D, bool LIST, bool MASS>
@@ -467,6 +469,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
             for (int s = 0; s < WIDE; ++s) r.k16[t][s] = *reinterpret_cast<const uint4 *>(p + 4 * t * D + 64 * s + 16 * hq);
             if (ODD) r.k8[t][0] = *reinterpret_cast<const uint2 *>(p + 4 * t * D + 64 * WIDE + 8 * hq);
         }
+        r.scales = *reinterpret_cast<const f32x2 *>(a.c.scales + (int64_t)page * 2);
     };
     auto load_v = [&](KvBlock<D> &r, int page) {
         const uint8_t *p = a.c.v + (int64_t)page * (KB * D) + x * KB + 16 * hq;
@@ -534,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
         pn = __builtin_amdgcn_readfirstlane(pn);
         f32x4 s[4];
         if (page >= 0) {
-            const float ks = a.c.scales[(int64_t)page * 2], vs = a.c.scales[(int64_t)page * 2 + 1];
+            const float ks = r.scales[0], half = r.scales[1] * T::VHALF;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -548,7 +551,6 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
             if (pn >= 0) load_k(r, pn);
             softmax(s, ks * a.scale2, j, (j + 1) * KB <= least);
             const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
-            const float half = vs * T::VHALF;
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
                 o[i] = T::mfma(bring8<T>(r.v[i].x, r.v[i].y, half), p0, o[i]);
@@ -661,7 +663,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     constexpr int DT = D / 32;                  // tiles of the second product
     constexpr int KP = D / 16;                  // pieces of a row of keys
     constexpr int LOADS = KB * D / 16 / 256 + (KB * D / 16 % 256 ? 1 : 0);  // pieces of a thread, of keys and of values
-    __shared__ __attribute__((aligned(16))) uint4 s_k[2][KB * D / 16], s_v[2][KB * D / 16];
+    __shared__ u32x4 s_k[2][KB * D / 16], s_v[2][KB * D / 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
     const int H = a.c.heads, g = a.g, units = a.tiles * H;
     const KvRange r = kv_plan(a.c, units, a.target, blockIdx.x, 0);
@@ -705,22 +707,24 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     // piece p of the keys lies at p of LDS; the piece of the row that it holds:
     auto k_piece = [](int token, int at) { return KP == 8 ? at ^ ((token & 3) | (token >> 4 & 1) << 2) : KP == 4 ? at ^ (token & 3) : at; };
     auto v_piece = [](int d, int at) { return at ^ (d >> 2 & 3); };
-    uint4 next_k[LOADS], next_v[LOADS];
+    u32x4 next_k[LOADS], next_v[LOADS];
+    f32x2 next_scales = {0.f, 0.f};
     auto fetch = [&](int page) {
-        const uint4 *pk = reinterpret_cast<const uint4 *>(a.c.k + (int64_t)page * (KB * D)), *pv = reinterpret_cast<const uint4 *>(a.c.v + (int64_t)page * (KB * D));
+        const u32x4 *pk = reinterpret_cast<const u32x4 *>(a.c.k + (int64_t)page * (KB * D)), *pv = reinterpret_cast<const u32x4 *>(a.c.v + (int64_t)page * (KB * D));
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int p = tid + 256 * i;
-            if (KB * D / 16 % 256 && p >= KB * D / 16) break;
+            if (KB * D / 16 % 256 && p >= KB * D / 16) continue;
             next_k[i] = pk[p / KP * KP + k_piece(p / KP, p % KP)];
             next_v[i] = pv[p / 4 * 4 + v_piece(p / 4, p % 4)];
         }
+        next_scales = *reinterpret_cast<const f32x2 *>(a.c.scales + (int64_t)page * 2);
     };
     auto stage = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int p = tid + 256 * i;
-            if (KB * D / 16 % 256 && p >= KB * D / 16) break;
+            if (KB * D / 16 % 256 && p >= KB * D / 16) continue;
             s_k[buf][p] = next_k[i];
             s_v[buf][p] = next_v[i];
         }
@@ -730,6 +734,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     // logits of a block become weights; z = s * scale
     auto softmax = [&](f32x16 (&s)[2], float scale, int j, bool all) {
         if (!all) {
+            asm volatile("");  // a branch: few blocks need the comparisons
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -785,16 +790,16 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     for (int j = from; j < paged; ++j) {
         const int next = __builtin_amdgcn_readfirstlane(after);
         after = j + 2 < paged ? kv_page(a.c, bh, j + 2) : -1;
+        const float ks = next_scales[0], vs = next_scales[1] * T::VHALF;
         if (next >= 0) fetch(next);
         if (page >= 0 && (MASS || j * KB < wmost)) {
-            const float ks = a.c.scales[(int64_t)page * 2], vs = a.c.scales[(int64_t)page * 2 + 1] * T::VHALF;
             f32x16 s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 s[t] = (f32x16)(0.f);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) {
-                    const uint4 w = s_k[buf][(kt + 32 * t) * KP + k_piece(kt + 32 * t, 2 * i + half)];
+                    const u32x4 w = s_k[buf][(kt + 32 * t) * KP + k_piece(kt + 32 * t, 2 * i + half)];
                     s[t] = T::mfma(bring8<T>(w.x, w.y, 1.f), q[2 * i], s[t]);
                     s[t] = T::mfma(bring8<T>(w.z, w.w, 1.f), q[2 * i + 1], s[t]);
                 }
@@ -807,7 +812,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
             for (int i = 0; i < DT; ++i)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const uint4 w = s_v[buf][(32 * i + x) * 4 + v_piece(32 * i + x, 2 * t + half)];
+                    const u32x4 w = s_v[buf][(32 * i + x) * 4 + v_piece(32 * i + x, 2 * t + half)];
                     o[i] = T::mfma(bring8<T>(w.x, w.y, vs), p[2 * t], o[i]);
                     o[i] = T::mfma(bring8<T>(w.z, w.w, vs), p[2 * t + 1], o[i]);
                 }
@@ -881,17 +886,18 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     }
 }
 
-// Joins the ranges of one row: a workgroup to a row of the tile, a thread to a dimension.
+// Joins the ranges of a long cache: 32 lanes to a row, eight rows to a workgroup.  A lane weighs one range at a time for its
+// row, then all of them add up four dimensions each; the loads of a round do not wait for one another.
 template <typename T, int D, int ROWS, bool LIST, bool MASS>
-__global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
+__global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a)
 {
-    const int H = a.c.heads, g = a.g, y = blockIdx.y, d = threadIdx.x;
-    int b, h, tile, token = 0, splits;
+    constexpr int PARTS = ROWS / 8;  // workgroups of a tile
+    const int H = a.c.heads, g = a.g, lane = threadIdx.x & 31, y = blockIdx.x % PARTS * 8 + threadIdx.x / 32;
+    const int64_t unit = blockIdx.x / PARTS;
+    const int h = (int)(unit % H), tile = (int)(unit / H % a.tiles);
+    int b, token = 0, splits;
     int64_t slot, step;
     if (LIST) {
-        const int64_t unit = blockIdx.x;
-        h = (int)(unit % H);
-        tile = (int)(unit / H % a.tiles);
         token = (int)(unit / ((int64_t)H * a.tiles) % a.n);
         b = (int)(unit / ((int64_t)H * a.tiles * a.n));
         splits = a.splits;
@@ -899,9 +905,7 @@ __global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
         step = a.units;
     } else {
         const int units = a.tiles * H;
-        h = blockIdx.x % H;
-        tile = blockIdx.x / H % a.tiles;
-        b = blockIdx.x / units;
+        b = (int)(unit / units);
         const KvRange r = kv_plan(a.c, units, a.target, -1, b);
         splits = r.splits;
         slot = r.first + tile * H + h;
@@ -910,22 +914,37 @@ __global__ __launch_bounds__(128) void k_kv_join(KvAttendArgs a)
     if (splits < 2) return;
     const int row = LIST ? token * g + tile * ROWS + y : tile * ROWS + y;
     const int qi = LIST ? token : row / g, hg = LIST ? tile * ROWS + y : row % g;
-    if ((LIST ? hg >= g : row >= a.n * g) || d >= D) return;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const int64_t at = (slot + s * step) * ROWS + y;
-        const float ms = a.part_ml[at * 2], ls = a.part_ml[at * 2 + 1], os = a.part_o[at * D + d];
-        const float top = fmaxf(m, ms), base = top == -INFINITY ? 0.f : top;
-        const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ms - base);
-        l = l * f0 + ls * f1;
-        o = o * f0 + os * f1;
+    if (LIST ? hg >= g : row >= a.n * g) return;
+    const int64_t first = slot * ROWS + y, next = step * ROWS;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < splits; s0 += 32) {
+        const int s = s0 + lane;
+        const float2 ml = s < splits ? *reinterpret_cast<const float2 *>(a.part_ml + (first + s * next) * 2) : make_float2(-INFINITY, 0.f);
+        float top = ml.x;
+        for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+        top = fmaxf(top, m);
+        const float base = top == -INFINITY ? 0.f : top, fade = __builtin_amdgcn_exp2f(m - base), weight = __builtin_amdgcn_exp2f(ml.x - base);
+        float sum = ml.y * weight;
+        for (int i = 16; i; i >>= 1) sum += __shfl_xor(sum, i);
+        l = l * fade + sum;
+        o *= fade;
         m = top;
+        const int many = min(32, splits - s0);
+        const float *from = a.part_o + (first + s0 * next) * D + 4 * (lane < D / 4 ? lane : 0);
+        for (int i0 = 0; i0 < many; i0 += 8) {
+            f32x4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i0 + i < many ? *reinterpret_cast<const f32x4 *>(from + (i0 + i) * next * D) : (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o += v[i] * __shfl(weight, (threadIdx.x & 32) + i0 + i);
+        }
     }
     const float f = l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
     const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg;
-    const typename T::x2 p = T::narrow(o * f, 0.f);
-    a.out[at * D + d] = (uint16_t)__builtin_bit_cast(uint32_t, p);
-    if (d == 0) {
+    const typename T::x2 p0 = T::narrow(o[0] * f, o[1] * f), p1 = T::narrow(o[2] * f, o[3] * f);
+    if (lane < D / 4) *reinterpret_cast<uint2 *>(a.out + at * D + 4 * lane) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+    if (lane == 0) {
         const float y2 = m + __builtin_amdgcn_logf(l);
         if (a.lse) a.lse[at] = y2 * 0.69314718055994531f;
         if (MASS) a.row_lse[((int64_t)b * H + h) * a.n * g + row] = y2;
@@ -961,8 +980,8 @@ __global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restri
 // Selection of blocks.  score(token, head, block) = largest over the group's query heads of
 //     key scale * sum_d max(q_d lo_d, q_d hi_d)  =  key scale * ( <max(q, 0), hi> + <min(q, 0), lo> ),
 // which no logit of the block exceeds (before the softmax scale).  k_kv_score takes it on the matrix cores: products of a query's
-// element and a code are exact in float32, their 2 D float32 additions are off by at most 2 D 2^-24 of the terms' sizes, of which
-// no sum is larger than key scale * 448 * sum_d |q_d|.  k_kv_pick takes the choice from these scores and bounds, and evaluates
+// element and a code are exact in float32, D of them are not zero, and their float32 additions, rounded or truncated, are off by at most
+// D 2^-23 of the sum of the terms' sizes, a second product of the same shape.  k_kv_pick takes the choice from these scores and bounds, and evaluates
 // the blocks that they leave open in float64, where products of at most 15 bits add up to the same sum in any order
 // unless a query's elements differ by more than 2^20 in size.
 // ------------------------------------------------------------------------------------------------
@@ -1017,21 +1036,25 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
     const int last = min(count, (turn + 1) * a.turns * a.tokens);  // tokens from there on see no less than the others
     if (last <= turn * a.turns * a.tokens || j0 >= min(max(0, len - count + last) / KB, a.c.blocks)) return;
     const int page = kv_page(a.c, bh, j0 + x);
-    typename T::x8 edge[2][KS];  // lo, hi
+    uint4 edge[2][KS];  // lo, hi
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const uint8_t *p = a.c.bounds + ((int64_t)max(page, 0) * 2 + e) * D;
 #pragma unroll
         for (int s = 0; s < WIDE; ++s) {
             const uint4 w = *reinterpret_cast<const uint4 *>(p + 64 * s + 16 * hq);
-            edge[e][2 * s] = bring8<T>(w.x, w.y, 1.f);
-            edge[e][2 * s + 1] = bring8<T>(w.z, w.w, 1.f);
+            edge[e][2 * s] = __builtin_bit_cast(uint4, bring8<T>(w.x, w.y, 1.f));
+            edge[e][2 * s + 1] = __builtin_bit_cast(uint4, bring8<T>(w.z, w.w, 1.f));
         }
         if (ODD) {
             const uint2 w = *reinterpret_cast<const uint2 *>(p + 64 * WIDE + 8 * hq);
-            edge[e][KS - 1] = bring8<T>(w.x, w.y, 1.f);
+            edge[e][KS - 1] = __builtin_bit_cast(uint4, bring8<T>(w.x, w.y, 1.f));
         }
     }
+    auto sizes = [](uint4 w) {
+        constexpr uint32_t mask = 0x7FFF7FFFu;
+        return __builtin_bit_cast(typename T::x8, make_uint4(w.x & mask, w.y & mask, w.z & mask, w.w & mask));
+    };
     const float own = page >= 0 ? a.c.scales[(int64_t)page * 2] : -1.f;
     float scale[4];
 #pragma unroll
@@ -1041,12 +1064,11 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
         const int token = tile * a.tokens + x / a.gp;
         const bool live = x / a.gp < a.tokens && token < count;
         f32x4 best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        float size = 0.f;  // largest sum of |q_d|
+        f32x4 size = {0.f, 0.f, 0.f, 0.f};  // largest sum of the terms' sizes
         bool odd = false;  // not a number anywhere
         for (int g0 = 0; g0 < a.g; g0 += 16) {
             const uint16_t *qp = a.q + b * a.qs[0] + (live ? token : 0) * a.qs[1] + ((int64_t)h * a.g + min(a.g - 1, g0 + x % a.gp)) * a.qs[2];
-            f32x4 s = {0.f, 0.f, 0.f, 0.f};
-            float sum = 0.f;
+            f32x4 s = {0.f, 0.f, 0.f, 0.f}, terms = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
@@ -1057,34 +1079,37 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
                 p.y = positive16(w.y);
                 p.z = positive16(w.z);
                 p.w = positive16(w.w);
-                s = T::mfma(edge[1][ks], __builtin_bit_cast(typename T::x8, p), s);
+                s = T::mfma(__builtin_bit_cast(typename T::x8, edge[1][ks]), __builtin_bit_cast(typename T::x8, p), s);
+                terms = T::mfma(sizes(edge[1][ks]), __builtin_bit_cast(typename T::x8, p), terms);
                 p.x ^= w.x;
                 p.y ^= w.y;
                 p.z ^= w.z;
                 p.w ^= w.w;
-                s = T::mfma(edge[0][ks], __builtin_bit_cast(typename T::x8, p), s);
-                for (uint32_t u : {w.x, w.y, w.z, w.w}) sum += fabsf(T::wide((uint16_t)u)) + fabsf(T::wide((uint16_t)(u >> 16)));
+                s = T::mfma(__builtin_bit_cast(typename T::x8, edge[0][ks]), __builtin_bit_cast(typename T::x8, p), s);
+                terms = T::mfma(sizes(edge[0][ks]), sizes(p), terms);
             }
-            size = fmaxf(size, row_sum(sum));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                odd = odd || s[i] != s[i];
+                odd = odd || s[i] != s[i] || terms[i] != terms[i];
                 best[i] = fmaxf(best[i], s[i]);
+                size[i] = fmaxf(size[i], terms[i]);
             }
         }
         for (int o = a.gp / 2; o; o >>= 1) {
-            size = fmaxf(size, __shfl_xor(size, o));
             odd = __shfl_xor((int)odd, o) || odd;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __shfl_xor(best[i], o));
+            for (int i = 0; i < 4; ++i) {
+                best[i] = fmaxf(best[i], __shfl_xor(best[i], o));
+                size[i] = fmaxf(size[i], __shfl_xor(size[i], o));
+            }
         }
         if (live && x % a.gp == 0) {
             uint64_t *to = a.scores + (((int64_t)b * a.n + token) * H + h) * a.c.blocks + j0 + 4 * hq;
-            // twice what the additions can be off by: the bound's own arithmetic, and the sums of score and bound, are rounded too
-            const float off = (4 * D + 16) * 5.9604645e-8f * 448.f * size;
+            // some more than D: the sum of sizes is as far off, and score plus bound are rounded once more
+            constexpr float off = (D + 16) * 1.1920929e-7f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float2 v = make_float2(best[i] * scale[i], off * scale[i]);
+                float2 v = make_float2(best[i] * scale[i], off * size[i] * scale[i]);
                 if (scale[i] < 0.f)
                     v = make_float2(0.f, -1.f);
                 else if (odd || !(fabsf(v.x) < INFINITY) || !(v.y < INFINITY))
@@ -1226,24 +1251,38 @@ struct Pick {
     }
 };
 
-// The score of one block in float64, by 16 lanes together: lane `part` of them has every 16th dimension.
-template <typename T>
-__device__ __forceinline__ double exact_score(const KvSelectArgs &a, const uint16_t *q, int page, int D, int part)
+// The score of one block in float64, by 16 lanes together: lane `part` of them has D / 16 dimensions in a row.
+template <typename T, int D>
+__device__ __forceinline__ double exact_score(const KvSelectArgs &a, const uint16_t *q, int page, int part)
 {
-    const uint8_t *lo = a.c.bounds + (int64_t)page * (2 * D), *hi = lo + D;
+    constexpr int N = D / 16;
+    const uint8_t *lo = a.c.bounds + (int64_t)page * (2 * D) + part * N, *hi = lo + D;
+    uint32_t codes[N];  // lo, and hi 16 bits higher
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const uint32_t x = reinterpret_cast<const uint16_t *>(lo)[i], y = reinterpret_cast<const uint16_t *>(hi)[i];
+        codes[2 * i] = (x & 0xFF) | (y & 0xFF) << 16;
+        codes[2 * i + 1] = x >> 8 | (y >> 8) << 16;
+    }
+    const float scale = a.c.scales[(int64_t)page * 2];
     double best = -INFINITY;
     bool odd = false;
+#pragma unroll 4
     for (int hg = 0; hg < a.g; ++hg) {
+        const uint32_t *row = reinterpret_cast<const uint32_t *>(q + hg * a.qs[2] + part * N);
         double sum = 0;
-        for (int d = part; d < D; d += 16) {
-            const float x = T::wide(q[hg * a.qs[2] + d]);
-            sum += (double)x * code_value(x > 0.f ? hi[d] : lo[d]);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const uint32_t w = row[i];
+            const float x = T::wide((uint16_t)w), y = T::wide((uint16_t)(w >> 16));
+            sum += (double)x * code_value(x > 0.f ? codes[2 * i] >> 16 : codes[2 * i]);
+            sum += (double)y * code_value(y > 0.f ? codes[2 * i + 1] >> 16 : codes[2 * i + 1]);
         }
         for (int o = 8; o; o >>= 1) sum += __shfl_xor(sum, o);
         odd = odd || sum != sum;
         best = fmax(best, sum);
     }
-    return odd ? NAN : best * (double)a.c.scales[(int64_t)page * 2];
+    return odd ? NAN : best * (double)scale;
 }
 
 // ROWS rows to a workgroup, WAVES waves to a row (one of the two is 1).  From the scores' intervals: no block below the w-th largest
@@ -1293,11 +1332,31 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
         upper.cut = least - 1;
         got = upper.walk(high, put);
     } else {
-        // no more than w upper ends lie above `sure`: a block whose lower end does is chosen
-        upper.find(a.w, high, s_sum, turn);
-        const uint32_t sure = upper.cut;
-        const int lane = threadIdx.x & 63;
+        // No more than w blocks have a lower end above `least` (or w have one from there on), so no more than w an upper end that lies
+        // by the widest interval above it: a block whose lower end does is chosen.  A few lie between: their exact
+        // scores are ranked against one another.
+        const int lane = threadIdx.x & 63, wave = Pick<uint32_t, WAVES, KPT>::wave();
+        float widest = 0.f;
+        for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
+            const int j = lower.from + k + lane;
+            float v, off = 0.f;
+            if (j < whole && !forced(j)) at(j, v, off);
+            widest = fmaxf(widest, off);
+        }
+        for (int o = 32; o; o >>= 1) widest = fmaxf(widest, __shfl_xor(widest, o));
+        __shared__ float s_widest[WAVES];
+        if (WAVES > 1) {
+            if (lane == 0) s_widest[wave] = widest;
+            __syncthreads();
+            for (int y = 0; y < WAVES; ++y) widest = fmaxf(widest, s_widest[y]);
+        }
+        const uint32_t bits = least >> 31 ? least & 0x7FFFFFFFu : ~least;  // the number whose key `least` is
+        const float edge = __uint_as_float(bits) + 2.5f * widest;
+        const bool firm = least < 0xFF800000u && least > 0x007FFFFFu && edge < INFINITY;  // a finite number, plus a finite one
+        const uint32_t sure = firm ? key_of(edge) : ~0u;
         const uint16_t *q = a.q + b * a.qs[0] + i * a.qs[1] + (int64_t)h * a.g * a.qs[2];
+        int sures = 0, opens = 0;
+        uint64_t open_key = 0;  // of the wave's open blocks, one to a lane
         for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
             const int j = lower.from + k + lane;
             const bool here = j < whole;
@@ -1305,7 +1364,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
             if (here) at(j, v, off);
             const uint32_t lo = here ? low(j) : 0, hi = here ? high(j) : 0;
             uint64_t key = hi < least ? 0 : lo > sure || lo == ~0u ? ~0ull : 2;
-            if (key == 2 && off == 0.f) key = key_of((double)v);  // a query of zeros
+            sures += __popcll(__ballot(key == ~0ull));
             uint64_t open = __ballot(key == 2);
             while (open) {  // four blocks at a time, 16 lanes to each
                 int bit[4], mine = -1;
@@ -1316,20 +1375,71 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
                     open &= open - 1;
                 }
                 const int page = mine >= 0 ? kv_page(a.c, (int64_t)b * H + h, lower.from + k + mine) : 0;
-                const double score = exact_score<T>(a, q, max(page, 0), D, lane & 15);
+                const double score = exact_score<T, D>(a, q, max(page, 0), lane & 15);
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const double one = __shfl(score, 16 * y);
-                    if (lane == bit[y]) key = key_of(one);
+                    const uint64_t one = key_of(__shfl(score, 16 * y));
+                    if (lane == bit[y]) key = one;
+                    if (bit[y] >= 0) {
+                        if (lane == opens) open_key = one;
+                        ++opens;
+                    }
                 }
             }
             if (here) scores[j] = key;  // a block's key takes its score's place
         }
-        auto key = [&](int j) { return scores[j]; };
-        Pick<uint64_t, WAVES, KPT> last;
-        last.load(whole, key);
-        last.find(a.w, key, s_sum, turn);
-        got = last.walk(key, put);
+        // open blocks of all waves, in their order
+        __shared__ uint64_t s_open[WAVES > 1 ? 64 * WAVES : 1];
+        __shared__ int s_found[2][WAVES];
+        bool fits = opens <= 64;
+        int before = 0, ahead = 0, need = a.w - sures;
+        if (WAVES > 1) {
+            if (lane == 0) {
+                s_found[0][wave] = sures;
+                s_found[1][wave] = opens;
+            }
+            if (lane < opens) s_open[64 * wave + lane] = open_key;
+            __syncthreads();
+            need = a.w;
+            for (int y = 0; y < WAVES; ++y) {
+                need -= s_found[0][y];
+                fits = fits && s_found[1][y] <= 64;
+            }
+            if (fits)
+                for (int y = 0; y < WAVES; ++y)
+                    for (int z = 0; z < s_found[1][y]; ++z) {
+                        const uint64_t other = s_open[64 * y + z];
+                        ahead += other > open_key || (other == open_key && (y < wave || (y == wave && z < lane)));
+                    }
+        } else if (fits) {
+            for (int z = 0; z < opens; ++z) {
+                const uint64_t other = __shfl(open_key, z);
+                ahead += other > open_key || (other == open_key && z < lane);
+            }
+        }
+        if (fits) {
+            const uint64_t wins = __ballot(lane < opens && ahead < need);
+            // the n-th open block of the wave wins if bit n is set
+            auto chosen = [&](int j) -> uint32_t { return scores[j] == ~0ull; };
+            for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
+                const int j = lower.from + k + lane;
+                const uint64_t key = j < whole ? scores[j] : 0;
+                const bool was_open = key != 0 && key != ~0ull;
+                const uint64_t open = __ballot(was_open);
+                const int nth = before + __popcll(open & ((1ull << lane) - 1));
+                if (was_open) scores[j] = wins >> (nth & 63) & 1 ? ~0ull : 0;
+                before += __popcll(open);
+            }
+            Pick<uint32_t, WAVES, KPT> last;
+            last.load(whole, chosen);
+            got = last.walk(chosen, put);
+        } else {  // many alike: all keys again
+            auto key = [&](int j) { return scores[j]; };
+            Pick<uint64_t, WAVES, KPT> last;
+            last.load(whole, key);
+            last.find(a.w, key, s_sum, turn);
+            got = last.walk(key, put);
+        }
     }
     for (int j = got + threadIdx.x % (64 * WAVES); j < a.w; j += 64 * WAVES) out[j] = -1;
 }
