@@ -1122,9 +1122,9 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // The `w` largest of `n` keys that are not zero, ties to the lower index.  WAVES waves take one row together; a wave holds up to 64 KPT
-// consecutive keys in registers.  The w-th largest key is found bit by bit from the top: a candidate is kept if at least w
-// keys reach it, counted by ballots, and the walk ends early once exactly w do, which keys of scores decide after some twenty
-// bits.  Rows longer than the registers read their keys again for every bit (KPT = 0).
+// consecutive keys in registers.  The w-th largest key is found by counting, with ballots, how many keys reach a number between two
+// bounds; where it would lie among evenly spread keys is tried first, and the walk ends once exactly w keys reach a
+// number: some eight counts for scores, two for a bit at most.  Rows longer than the registers read their keys again for every bit (KPT = 0).
 // ------------------------------------------------------------------------------------------------
 template <typename U, int WAVES, int KPT>
 struct Pick {
@@ -1151,14 +1151,12 @@ struct Pick {
     __device__ __forceinline__ int reach(U x, Key key, int (&s_sum)[2][WAVES], int turn) const
     {
         int c = 0;
+        if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) {
-            if (KPT && from + 64 * i >= n) break;
-            if (KPT) {
-                c += __popcll(__ballot(keys[i] >= x));
-            } else {
-                for (int k = 0; k < span && from + k < n; k += 64) c += __popcll(__ballot(at(k / 64, key) >= x));
-            }
+            for (int i = 0; i < KPT; ++i)
+                if (from + 64 * i < n) c += __popcll(__ballot(keys[i] >= x));
+        } else {
+            for (int k = 0; k < span && from + k < n; k += 64) c += __popcll(__ballot(at(k / 64, key) >= x));
         }
         if (WAVES == 1) return c;
         if (lane() == 0) s_sum[turn][wave()] = c;
@@ -1186,21 +1184,70 @@ struct Pick {
     template <typename Key>
     __device__ __forceinline__ void find(int w, Key key, int (&s_sum)[2][WAVES], int &turn)
     {
-        const int have = reach(1, key, s_sum, turn ^= 1);
-        if (have <= w) return;  // no more than asked for: all of them
-        U x = 0;
-        for (int bit = 8 * (int)sizeof(U) - 1; bit >= 0; --bit) {
-            const U y = x | (U)1 << bit;
-            const int c = reach(y, key, s_sum, turn ^= 1);
+        int cl = reach(1, key, s_sum, turn ^= 1);
+        if (cl <= w) return;  // no more than asked for: all of them
+        // more than w keys reach l, fewer than w reach r
+        const U all = (U)~(U)0;
+        int cr = reach(all, key, s_sum, turn ^= 1);  // those that are always chosen
+        if (cr >= w) {
+            cut = all;
+            ties = w;
+            return;
+        }
+        U l = all, r = 0;  // smallest and largest of the others
+        auto ends = [&](U k) {
+            if (k != 0 && k != all) {
+                l = k < l ? k : l;
+                r = k > r ? k : r;
+            }
+        };
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) ends(keys[i]);
+        } else {
+            for (int k = 0; k < span && from + k < n; k += 64) ends(at(k / 64, key));
+        }
+        for (int o = 32; o; o >>= 1) {
+            const U x = __shfl_xor(l, o), y = __shfl_xor(r, o);
+            l = x < l ? x : l;
+            r = y > r ? y : r;
+        }
+        if (WAVES > 1) {
+            __shared__ U s_ends[2][WAVES];
+            if (lane() == 0) {
+                s_ends[0][wave()] = l;
+                s_ends[1][wave()] = r;
+            }
+            __syncthreads();
+            for (int i = 0; i < WAVES; ++i) {
+                l = s_ends[0][i] < l ? s_ends[0][i] : l;
+                r = s_ends[1][i] > r ? s_ends[1][i] : r;
+            }
+        }
+        ++r;
+        for (int turns = 0; r - l > 1; ++turns) {
+            // where the w-th key would lie if they were spread evenly, and the middle, in turn
+            const U gap = r - l;
+            U step = gap / 2;
+            if (turns % 2 == 0) step = (U)((float)gap * ((cl - w + 0.5f) / (float)(cl - cr)));
+            step = step < 1 ? 1 : step > gap - 1 ? gap - 1 : step;
+            const U x = l + step;
+            const int c = reach(x, key, s_sum, turn ^= 1);
             if (c == w) {
-                cut = y - 1;
+                cut = x - 1;
                 return;
             }
-            if (c > w) x = y;
+            if (c > w) {
+                l = x;
+                cl = c;
+            } else {
+                r = x;
+                cr = c;
+            }
         }
-        // x is the w-th largest key, and more than one equals it
-        cut = x;
-        ties = w - (x == (U)~(U)0 ? 0 : reach(x + 1, key, s_sum, turn ^= 1));
+        // l is the w-th largest key, and more than one equals it
+        cut = l;
+        ties = w - cr;
     }
 
     // Calls put(j, place, chosen) for every j < n, place = how many of its kind come before it; returns the number of chosen ones.
@@ -1210,10 +1257,19 @@ struct Pick {
         __shared__ int s_kind[2][WAVES];
         int over = 0, same = 0, all = 0;
         if (WAVES > 1) {
-            for (int k = 0; k < span && from + k < n; k += 64) {
-                const U v = at(k / 64, key);
-                over += __popcll(__ballot(v > cut));
-                same += __popcll(__ballot(v != 0 && v == cut));
+            if constexpr (KPT > 0) {
+#pragma unroll
+                for (int i = 0; i < KPT; ++i)
+                    if (from + 64 * i < n) {
+                        over += __popcll(__ballot(keys[i] > cut));
+                        same += __popcll(__ballot(keys[i] != 0 && keys[i] == cut));
+                    }
+            } else {
+                for (int k = 0; k < span && from + k < n; k += 64) {
+                    const U v = at(k / 64, key);
+                    over += __popcll(__ballot(v > cut));
+                    same += __popcll(__ballot(v != 0 && v == cut));
+                }
             }
             if (lane() == 0) {
                 s_kind[0][wave()] = over;
@@ -1233,19 +1289,22 @@ struct Pick {
             all = so + min(ss, ties);
         }
         const uint64_t below = (1ull << lane()) - 1;
+        auto round = [&](int k, U v) {
+            const int j = from + k + lane();
+            const uint64_t bo = __ballot(v > cut), bs = __ballot(v != 0 && v == cut);
+            const int os = same + __popcll(bs & below);
+            const bool take = v > cut || (v != 0 && v == cut && os < ties);
+            const int place = over + __popcll(bo & below) + min(os, ties);
+            if (j < n) put(j, take ? place : j - place, take);
+            over += __popcll(bo);
+            same += __popcll(bs);
+        };
+        if constexpr (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < (KPT ? KPT : 1); ++i) {
-            for (int k = KPT ? 64 * i : 0; k < (KPT ? 64 * i + 1 : span) && from + k < n; k += 64) {
-                const int j = from + k + lane();
-                const U v = KPT ? keys[i] : at(k / 64, key);
-                const uint64_t bo = __ballot(v > cut), bs = __ballot(v != 0 && v == cut);
-                const int os = same + __popcll(bs & below);
-                const bool take = v > cut || (v != 0 && v == cut && os < ties);
-                const int place = over + __popcll(bo & below) + min(os, ties);
-                if (j < n) put(j, take ? place : j - place, take);
-                over += __popcll(bo);
-                same += __popcll(bs);
-            }
+            for (int i = 0; i < KPT; ++i)
+                if (from + 64 * i < n) round(64 * i, keys[i]);
+        } else {
+            for (int k = 0; k < span && from + k < n; k += 64) round(k, at(k / 64, key));
         }
         return WAVES == 1 ? over + min(same, ties) : all;
     }
@@ -1267,20 +1326,31 @@ __device__ __forceinline__ double exact_score(const KvSelectArgs &a, const uint1
     const float scale = a.c.scales[(int64_t)page * 2];
     double best = -INFINITY;
     bool odd = false;
-#pragma unroll 4
-    for (int hg = 0; hg < a.g; ++hg) {
-        const uint32_t *row = reinterpret_cast<const uint32_t *>(q + hg * a.qs[2] + part * N);
-        double sum = 0;
+    for (int h0 = 0; h0 < a.g; h0 += 4) {  // four heads at a time, the last one again where there are fewer
+        uint32_t w[4][N / 2];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const uint32_t w = row[i];
-            const float x = T::wide((uint16_t)w), y = T::wide((uint16_t)(w >> 16));
-            sum += (double)x * code_value(x > 0.f ? codes[2 * i] >> 16 : codes[2 * i]);
-            sum += (double)y * code_value(y > 0.f ? codes[2 * i + 1] >> 16 : codes[2 * i + 1]);
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) w[y][i] = reinterpret_cast<const uint32_t *>(q + min(h0 + y, a.g - 1) * a.qs[2] + part * N)[i];
+        double sum[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            sum[y] = 0;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float x0 = T::wide((uint16_t)w[y][i]), x1 = T::wide((uint16_t)(w[y][i] >> 16));
+                sum[y] += (double)x0 * code_value(x0 > 0.f ? codes[2 * i] >> 16 : codes[2 * i]);
+                sum[y] += (double)x1 * code_value(x1 > 0.f ? codes[2 * i + 1] >> 16 : codes[2 * i + 1]);
+            }
         }
-        for (int o = 8; o; o >>= 1) sum += __shfl_xor(sum, o);
-        odd = odd || sum != sum;
-        best = fmax(best, sum);
+        for (int o = 8; o; o >>= 1)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) sum[y] += __shfl_xor(sum[y], o);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            odd = odd || sum[y] != sum[y];
+            best = fmax(best, sum[y]);
+        }
     }
     return odd ? NAN : best * (double)scale;
 }
@@ -1300,51 +1370,49 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
     int turn = 0;
     uint64_t *scores = a.scores + row * a.c.blocks;
     int32_t *out = a.lists + row * a.w;
-    auto at = [&](int j, float &v, float &off) {
-        const uint64_t u = scores[j];
-        v = __uint_as_float((uint32_t)u);
-        off = __uint_as_float((uint32_t)(u >> 32));
-    };
     auto forced = [&](int j) { return j < a.sink || j >= whole - a.recent; };
-    auto low = [&](int j) -> uint32_t {
-        float v, off;
-        at(j, v, off);
+    auto low_of = [&](int j, uint64_t u) -> uint32_t {
+        const float v = __uint_as_float((uint32_t)u), off = __uint_as_float((uint32_t)(u >> 32));
         if (off < 0.f) return 0;
         return forced(j) ? ~0u : off == INFINITY ? 1 : key_of(v - off);
     };
-    auto high = [&](int j) -> uint32_t {
-        float v, off;
-        at(j, v, off);
+    auto high_of = [&](int j, uint64_t u) -> uint32_t {
+        const float v = __uint_as_float((uint32_t)u), off = __uint_as_float((uint32_t)(u >> 32));
         if (off < 0.f) return 0;
         return forced(j) ? ~0u : off == INFINITY ? ~0u - 1 : key_of(v + off);
     };
+    auto low = [&](int j) { return low_of(j, scores[j]); };
+    auto high = [&](int j) { return high_of(j, scores[j]); };
     auto put = [&](int j, int place, bool take) {
         if (take) out[place] = j;
     };
-    int got;
+    const int lane = threadIdx.x & 63, wave = Pick<uint32_t, WAVES, KPT>::wave();
+    const uint16_t *q = a.q + b * a.qs[0] + i * a.qs[1] + (int64_t)h * a.g * a.qs[2];
+    int got = -1;
     Pick<uint32_t, WAVES, KPT> lower, upper;
     lower.load(whole, low);
+    upper.load(whole, high);
     lower.find(a.w, low, s_sum, turn);
     // w blocks reach `least` with their lower ends: one whose upper end does not cannot be chosen
     const uint32_t least = lower.ties ? lower.cut : lower.cut + 1;
-    upper.load(whole, high);
     if (upper.reach(least, high, s_sum, turn ^= 1) <= a.w) {
         upper.cut = least - 1;
         got = upper.walk(high, put);
-    } else {
+    } else if constexpr (KPT > 0) {
         // No more than w blocks have a lower end above `least` (or w have one from there on), so no more than w an upper end that lies
-        // by the widest interval above it: a block whose lower end does is chosen.  A few lie between: their exact
-        // scores are ranked against one another.
-        const int lane = threadIdx.x & 63, wave = Pick<uint32_t, WAVES, KPT>::wave();
+        // by the widest interval above it: a block whose lower end does is chosen.  The few between, up to 64 of a wave, are
+        // evaluated and ranked against one another.
+        __shared__ float s_widest[WAVES];
+        __shared__ uint64_t s_open[ROWS * WAVES][64];
+        __shared__ int s_found[2][WAVES];
+        int *list = reinterpret_cast<int *>(s_open[threadIdx.x >> 6]);  // the wave's open blocks
         float widest = 0.f;
-        for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
-            const int j = lower.from + k + lane;
-            float v, off = 0.f;
-            if (j < whole && !forced(j)) at(j, v, off);
-            widest = fmaxf(widest, off);
+#pragma unroll
+        for (int y = 0; y < KPT; ++y) {
+            const int j = lower.from + 64 * y + lane;
+            if (j < whole && !forced(j)) widest = fmaxf(widest, __uint_as_float((uint32_t)(scores[j] >> 32)));
         }
         for (int o = 32; o; o >>= 1) widest = fmaxf(widest, __shfl_xor(widest, o));
-        __shared__ float s_widest[WAVES];
         if (WAVES > 1) {
             if (lane == 0) s_widest[wave] = widest;
             __syncthreads();
@@ -1354,17 +1422,79 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
         const float edge = __uint_as_float(bits) + 2.5f * widest;
         const bool firm = least < 0xFF800000u && least > 0x007FFFFFu && edge < INFINITY;  // a finite number, plus a finite one
         const uint32_t sure = firm ? key_of(edge) : ~0u;
-        const uint16_t *q = a.q + b * a.qs[0] + i * a.qs[1] + (int64_t)h * a.g * a.qs[2];
         int sures = 0, opens = 0;
-        uint64_t open_key = 0;  // of the wave's open blocks, one to a lane
+#pragma unroll
+        for (int y = 0; y < KPT; ++y) {
+            const bool chosen = upper.keys[y] >= least && upper.keys[y] != 0 && (lower.keys[y] > sure || lower.keys[y] == ~0u);
+            const uint64_t open = __ballot(upper.keys[y] >= least && !chosen);
+            const int nth = opens + __popcll(open & ((1ull << lane) - 1));
+            if ((open >> lane & 1) && nth < 64) list[nth] = lower.from + 64 * y + lane;
+            // from here on: 0, 1 chosen, 2 open
+            upper.keys[y] = chosen ? 1 : open >> lane & 1 ? 2 : 0;
+            sures += __popcll(__ballot(chosen));
+            opens += __popcll(open);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        bool fits = opens <= 64;
+        int need = a.w - sures, ahead = 0;
+        uint64_t own = 0;  // key of the wave's lane-th open block
+        if (fits) {
+            const int mine = lane < opens ? list[lane] : -1;
+            for (int z = 0; z < opens; z += 4) {  // four blocks at a time, 16 lanes to each
+                const int j = __shfl(mine, min(z + lane / 16, 63));
+                const int page = j >= 0 && z + lane / 16 < opens ? kv_page(a.c, (int64_t)b * H + h, j) : 0;
+                const uint64_t key = key_of(exact_score<T, D>(a, q, max(page, 0), lane & 15));
+                const uint64_t here = __shfl(key, (lane - z) * 16 & 63);
+                if (lane >= z && lane < z + 4) own = here;
+            }
+        }
+        if (WAVES > 1) {
+            __syncthreads();
+            if (lane == 0) {
+                s_found[0][wave] = sures;
+                s_found[1][wave] = opens;
+            }
+            if (lane < opens) s_open[wave][lane] = own;
+            __syncthreads();
+            need = a.w;
+            for (int y = 0; y < WAVES; ++y) {
+                need -= s_found[0][y];
+                fits = fits && s_found[1][y] <= 64;
+            }
+            if (fits)
+                for (int y = 0; y < WAVES; ++y)
+                    for (int z = 0; z < s_found[1][y]; ++z) {
+                        const uint64_t other = s_open[y][z];
+                        ahead += other > own || (other == own && (y < wave || (y == wave && z < lane)));
+                    }
+        } else if (fits) {
+            for (int z = 0; z < opens; ++z) {
+                const uint64_t other = __shfl(own, z);
+                ahead += other > own || (other == own && z < lane);
+            }
+        }
+        if (fits) {
+            const uint64_t wins = __ballot(lane < opens && ahead < need);  // bit n: the wave's n-th open block
+            int before = 0;
+#pragma unroll
+            for (int y = 0; y < KPT; ++y) {
+                const uint64_t open = __ballot(upper.keys[y] == 2);
+                const int nth = before + __popcll(open & ((1ull << lane) - 1));
+                if (upper.keys[y] == 2) upper.keys[y] = wins >> (nth & 63) & 1;
+                before += __popcll(open);
+            }
+            upper.cut = 0;
+            upper.ties = 0;
+            got = upper.walk(high, put);
+        }
+    }
+    if (got < 0) {  // many blocks alike: the exact scores of all that may be chosen, in the place of their bounds
         for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
             const int j = lower.from + k + lane;
-            const bool here = j < whole;
-            float v = 0.f, off = -1.f;
-            if (here) at(j, v, off);
-            const uint32_t lo = here ? low(j) : 0, hi = here ? high(j) : 0;
-            uint64_t key = hi < least ? 0 : lo > sure || lo == ~0u ? ~0ull : 2;
-            sures += __popcll(__ballot(key == ~0ull));
+            uint64_t key = 0;
+            if (j < whole) key = high(j) < least ? 0 : forced(j) ? ~0ull : 2;
+            if (key == 2 && scores[j] >> 32 == 0) key = key_of((double)__uint_as_float((uint32_t)scores[j]));  // a query of zeros
             uint64_t open = __ballot(key == 2);
             while (open) {  // four blocks at a time, 16 lanes to each
                 int bit[4], mine = -1;
@@ -1375,71 +1505,20 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
                     open &= open - 1;
                 }
                 const int page = mine >= 0 ? kv_page(a.c, (int64_t)b * H + h, lower.from + k + mine) : 0;
-                const double score = exact_score<T, D>(a, q, max(page, 0), lane & 15);
+                const uint64_t score = key_of(exact_score<T, D>(a, q, max(page, 0), lane & 15));
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const uint64_t one = key_of(__shfl(score, 16 * y));
+                    const uint64_t one = __shfl(score, 16 * y);
                     if (lane == bit[y]) key = one;
-                    if (bit[y] >= 0) {
-                        if (lane == opens) open_key = one;
-                        ++opens;
-                    }
                 }
             }
-            if (here) scores[j] = key;  // a block's key takes its score's place
+            if (j < whole) scores[j] = key;
         }
-        // open blocks of all waves, in their order
-        __shared__ uint64_t s_open[WAVES > 1 ? 64 * WAVES : 1];
-        __shared__ int s_found[2][WAVES];
-        bool fits = opens <= 64;
-        int before = 0, ahead = 0, need = a.w - sures;
-        if (WAVES > 1) {
-            if (lane == 0) {
-                s_found[0][wave] = sures;
-                s_found[1][wave] = opens;
-            }
-            if (lane < opens) s_open[64 * wave + lane] = open_key;
-            __syncthreads();
-            need = a.w;
-            for (int y = 0; y < WAVES; ++y) {
-                need -= s_found[0][y];
-                fits = fits && s_found[1][y] <= 64;
-            }
-            if (fits)
-                for (int y = 0; y < WAVES; ++y)
-                    for (int z = 0; z < s_found[1][y]; ++z) {
-                        const uint64_t other = s_open[64 * y + z];
-                        ahead += other > open_key || (other == open_key && (y < wave || (y == wave && z < lane)));
-                    }
-        } else if (fits) {
-            for (int z = 0; z < opens; ++z) {
-                const uint64_t other = __shfl(open_key, z);
-                ahead += other > open_key || (other == open_key && z < lane);
-            }
-        }
-        if (fits) {
-            const uint64_t wins = __ballot(lane < opens && ahead < need);
-            // the n-th open block of the wave wins if bit n is set
-            auto chosen = [&](int j) -> uint32_t { return scores[j] == ~0ull; };
-            for (int k = 0; k < lower.span && lower.from + k < whole; k += 64) {
-                const int j = lower.from + k + lane;
-                const uint64_t key = j < whole ? scores[j] : 0;
-                const bool was_open = key != 0 && key != ~0ull;
-                const uint64_t open = __ballot(was_open);
-                const int nth = before + __popcll(open & ((1ull << lane) - 1));
-                if (was_open) scores[j] = wins >> (nth & 63) & 1 ? ~0ull : 0;
-                before += __popcll(open);
-            }
-            Pick<uint32_t, WAVES, KPT> last;
-            last.load(whole, chosen);
-            got = last.walk(chosen, put);
-        } else {  // many alike: all keys again
-            auto key = [&](int j) { return scores[j]; };
-            Pick<uint64_t, WAVES, KPT> last;
-            last.load(whole, key);
-            last.find(a.w, key, s_sum, turn);
-            got = last.walk(key, put);
-        }
+        auto key = [&](int j) { return scores[j]; };
+        Pick<uint64_t, WAVES, KPT> last;
+        last.load(whole, key);
+        last.find(a.w, key, s_sum, turn);
+        got = last.walk(key, put);
     }
     for (int j = got + threadIdx.x % (64 * WAVES); j < a.w; j += 64 * WAVES) out[j] = -1;
 }
