@@ -95,6 +95,7 @@ int enter_device(const etf_ctx *ctx)
 // How an attention call is cut up, and where its workspace's arrays lie.
 struct AttendPlan {
     bool many = false;  // tiles of 128 rows instead of 16
+    bool solo = false;  // listed blocks: a wave to a unit
     int tiles = 0, splits = 1, rows = 16;
     int64_t units = 0, target = 0, grid = 0, o_ml = 0, o_row = 0, o_block = 0, total = 0;
 };
@@ -109,7 +110,8 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         p.units = (int64_t)c->batch * n * c->heads * p.tiles;
         // enough workgroups for the card, none with less than a block to a wave
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 768 / std::max<int64_t>(1, p.units)));
-        p.grid = p.units * p.splits;
+        p.solo = p.units >= 2048;
+        p.grid = p.solo ? (p.units + 3) / 4 : p.units * p.splits;
     } else {
         p.many = rows > 64;
         p.rows = p.many ? 128 : 16;
@@ -145,7 +147,14 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
             return ETF_OK;
         }
     }
-    hipLaunchKernelGGL((k_kv_attend<T, D, LIST, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
+    if constexpr (LIST) {
+        if (p.solo) {
+            hipLaunchKernelGGL((k_kv_attend<T, D, true, false, true>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
+            LAUNCH_CHECK(ctx, "k_kv_attend");
+            return ETF_OK;
+        }
+    }
+    hipLaunchKernelGGL((k_kv_attend<T, D, LIST, MASS, false>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_attend");
     if (LIST ? p.splits > 1 : p.target > 0) {
         const int64_t units = LIST ? p.units : a.c.batch * p.units;

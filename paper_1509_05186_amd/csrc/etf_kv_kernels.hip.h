@@ -277,8 +277,10 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
 // of one key/value head.  s^T = K q^T and o^T = V^T p^T on v_mfma_f32_16x16x32: a lane's column is a row of the tile, so
 // the running maximum and sum are the lane's own and the tile of s^T is, register for register, the operand p^T of the
 // second product (which token of the block stands in which row of s^T is chosen so: row m of tile t is token
-// 16 (m / 4) + 4 t + m % 4).  Keys and values go from memory into registers, 16 bytes to a lane: the next block's keys
-// are asked for when this one's are used up, the values likewise.  A wave takes every fourth block of its workgroup's
+// 16 (m / 4) + 4 t + m % 4).  Keys and values go straight from memory to LDS, 1 KB contiguous to a load, and from there as operands
+// into registers (loaded as operands, whose neighbouring lanes lie a row apart, every lane of a load is an access of its own:
+// 10.7 instead of 13.2 TB/s from the second-level cache); the next block's keys are asked for as soon as this one's are in
+// registers, the values likewise, so that a wave always has a block on its way.  A wave takes every fourth block of its workgroup's
 // range; the four join through LDS, ranges of a long cache through memory (k_kv_join).
 // ------------------------------------------------------------------------------------------------
 struct KvAttendArgs {
@@ -354,33 +356,121 @@ __device__ __forceinline__ float row_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// A block's keys and values as they lie in a page: what one lane feeds into the products.
-template <int D>
-struct KvBlock {
-    uint4 k16[4][D / 64];
-    uint2 k8[4][1];
-    uint4 v[D / 16];
-    f32x2 scales;
-};
+// Where the 16-byte piece `at` of a row of keys (a token's) or values (a dimension's) stands in its row of LDS: lanes that read
+// together hit all banks.  Its own inverse but for rows of six pieces (BACK: which piece stands at `at`).
+template <int D, bool BACK>
+__device__ __forceinline__ int k_place(int token, int at)
+{
+    if constexpr (D == 96) return (at + (BACK ? 6 - (token >> 4) : token >> 4)) % 6;
+    return at ^ (D == 128 ? (token >> 1 & 1) | (token >> 4) << 1 : token >> 4);
+}
+__device__ __forceinline__ int v_place(int d, int at) { return at ^ (d >> 2 & 3); }
 
-template <typename T, int D, bool LIST, bool MASS>
+// 16 bytes to a lane from `from` to the 1 KB of LDS at `to`, in the order of the lanes
+__device__ __forceinline__ void load_lds(const void *from, void *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+// waits until no more than `left` of the wave's loads are on their way
+#define KV_WAIT_LOADS(left) asm volatile("s_waitcnt vmcnt(" #left ")" ::: "memory")
+__device__ __forceinline__ void wait_loads(int left)
+{
+    switch (left) {
+        case 8: KV_WAIT_LOADS(8); break;
+        case 6: KV_WAIT_LOADS(6); break;
+        case 4: KV_WAIT_LOADS(4); break;
+        default: KV_WAIT_LOADS(0);
+    }
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+
+// Reads of LDS that have arrived when the block ends (the compiler, which does not see that the loads into LDS and these
+// reads are ordered by the waits above, would wait for every load on its way before each of them).
+// Eight rows of 1 KB apart, or six, or four: the values of a lane.
+template <int N>
+__device__ __forceinline__ void read_v(uint32_t at, u32x4 (&v)[N])
+{
+    if constexpr (N == 8)
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %8 offset:3072\n\t"
+                     "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %8 offset:5120\n\tds_read_b128 %6, %8 offset:6144\n\tds_read_b128 %7, %8 offset:7168\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+                     : "v"(at)
+                     : "memory");
+    else if constexpr (N == 6)
+        asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %6 offset:1024\n\tds_read_b128 %2, %6 offset:2048\n\tds_read_b128 %3, %6 offset:3072\n\t"
+                     "ds_read_b128 %4, %6 offset:4096\n\tds_read_b128 %5, %6 offset:5120\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5])
+                     : "v"(at)
+                     : "memory");
+    else
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %4 offset:3072\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                     : "v"(at)
+                     : "memory");
+}
+// The keys of a lane: four tokens, four apart; of each the pieces at `at` and (128 dimensions) `more`, or half a piece at `more` (96).
+template <int D>
+struct KvKeys {
+    u32x4 wide[4][D / 64];
+    uint2 odd[4];
+};
+template <int D>
+__device__ __forceinline__ void read_k(uint32_t at, uint32_t more, KvKeys<D> &k)
+{
+    if constexpr (D == 128) {
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %8 offset:512\n\tds_read_b128 %3, %9 offset:512\n\t"
+                     "ds_read_b128 %4, %8 offset:1024\n\tds_read_b128 %5, %9 offset:1024\n\tds_read_b128 %6, %8 offset:1536\n\tds_read_b128 %7, %9 offset:1536\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(k.wide[0][0]), "=&v"(k.wide[0][1]), "=&v"(k.wide[1][0]), "=&v"(k.wide[1][1]), "=&v"(k.wide[2][0]), "=&v"(k.wide[2][1]),
+                       "=&v"(k.wide[3][0]), "=&v"(k.wide[3][1])
+                     : "v"(at), "v"(more)
+                     : "memory");
+    } else if constexpr (D == 96) {
+        uint64_t o[4];
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b64 %1, %9\n\tds_read_b128 %2, %8 offset:384\n\tds_read_b64 %3, %9 offset:384\n\t"
+                     "ds_read_b128 %4, %8 offset:768\n\tds_read_b64 %5, %9 offset:768\n\tds_read_b128 %6, %8 offset:1152\n\tds_read_b64 %7, %9 offset:1152\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(k.wide[0][0]), "=&v"(o[0]), "=&v"(k.wide[1][0]), "=&v"(o[1]), "=&v"(k.wide[2][0]), "=&v"(o[2]), "=&v"(k.wide[3][0]), "=&v"(o[3])
+                     : "v"(at), "v"(more)
+                     : "memory");
+        for (int t = 0; t < 4; ++t) k.odd[t] = make_uint2((uint32_t)o[t], (uint32_t)(o[t] >> 32));
+    } else {
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:256\n\tds_read_b128 %2, %4 offset:512\n\tds_read_b128 %3, %4 offset:768\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(k.wide[0][0]), "=&v"(k.wide[1][0]), "=&v"(k.wide[2][0]), "=&v"(k.wide[3][0])
+                     : "v"(at)
+                     : "memory");
+    }
+}
+
+// SOLO: every wave of a workgroup has a unit of its own (listed blocks, enough units for the card): nothing to join.
+template <typename T, int D, bool LIST, bool MASS, bool SOLO>
 __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
 {
+    static_assert(!SOLO || (LIST && !MASS), "units of a wave are listed ones");
     constexpr int KS = D / 32;  // steps of the first product
     constexpr int DT = D / 16;  // tiles of the second
     constexpr int WIDE = D / 64, ODD = D % 64 / 32;
     constexpr int OROW = D + 4;
-    __shared__ float s_o[4][16][OROW];
-    __shared__ float s_ml[4][16][2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 15, hq = lane >> 4;
+    constexpr int HALF = KB * D;            // bytes of a block's keys, of its values
+    constexpr int LOADS = HALF / 1024;      // loads for either
+    constexpr int JOIN = 4 * 16 * (OROW + 2) * 4;
+    // a wave's block on its way; afterwards the waves' results
+    __shared__ __attribute__((aligned(1024))) uint8_t s_all[8 * HALF > JOIN || SOLO ? 8 * HALF : JOIN];
+    float(*s_o)[16][OROW] = reinterpret_cast<float(*)[16][OROW]>(s_all);
+    float(*s_ml)[16][2] = reinterpret_cast<float(*)[16][2]>(s_all + 4 * 16 * OROW * 4);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), x = lane & 15, hq = lane >> 4;
     const int H = a.c.heads, g = a.g;
     int b, h, tile, token = 0, splits, from, to;
     int64_t slot;
     if (LIST) {
         splits = a.splits;
-        const int64_t unit = blockIdx.x % a.units;
-        const int split = (int)(blockIdx.x / a.units);
-        slot = blockIdx.x;
+        slot = SOLO ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+        if (SOLO && slot >= a.units) return;
+        const int64_t unit = SOLO ? slot : blockIdx.x % a.units;
+        const int split = SOLO ? 0 : (int)(blockIdx.x / a.units);
         h = (int)(unit % H);
         tile = (int)(unit / H % a.tiles);
         token = (int)(unit / ((int64_t)H * a.tiles) % a.n);
@@ -440,41 +530,55 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
     for (int i = 0; i < DT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    // item u of the range: block j of the cache and the page it lies in (-1: none), or the open block
-    auto item = [&](int u, int &j, int &page, bool &open) {
-        open = false;
-        page = -1;
+    // A wave's items, every STEPth of the range: number u of them is block j of the cache and the page it lies in (-1: none, -2: the
+    // open block).  64 of them are looked up together, one to a lane.
+    constexpr int STEP = SOLO ? 1 : 4;
+    const int start = SOLO ? from : from + wave, many = start < to ? (to - start + STEP - 1) / STEP : 0;
+    int js = 0, ps = -1;
+    f32x2 ss = {0.f, 0.f};
+    auto look = [&](int u0) {
+        const int u = start + (u0 + lane) * STEP;
+        js = 0;
+        ps = -1;
+        if (u >= to) return;
+        bool open = false;
         if (LIST) {
             if (u == a.w) {  // the block that the token sees a part of
-                j = whole;
+                js = whole;
                 if (most % KB == 0) return;
-                open = j == nb;
+                open = js == nb;
             } else {
-                j = a.lists[(((int64_t)b * a.n + token) * H + h) * a.w + u];
-                if (j < 0 || j >= whole) return;
+                js = a.lists[(((int64_t)b * a.n + token) * H + h) * a.w + u];
+                if (js < 0 || js >= whole) return;
             }
         } else {
-            j = u;
-            open = j == nb;
+            js = u;
+            open = js == nb;
         }
-        if (!open) page = kv_page(a.c, bh, j);
+        ps = open ? -2 : kv_page(a.c, bh, js);
+        if (ps >= 0) ss = *reinterpret_cast<const f32x2 *>(a.c.scales + (int64_t)ps * 2);
     };
 
     const int kt = 16 * (x / 4) + x % 4;  // this lane's token of key tile 0
-    auto load_k = [&](KvBlock<D> &r, int page) {
-        const uint8_t *p = a.c.k + (int64_t)page * (KB * D) + kt * D;
+    uint8_t *s_k = s_all + wave * (2 * HALF), *s_v = s_k + HALF;
+    const uint32_t k_at = lds_address(s_k) + kt * D + 16 * k_place<D, false>(kt, hq);
+    const uint32_t k_more = D == 128 ? k_at ^ 64 : lds_address(s_k) + kt * D + 16 * k_place<D, false>(kt, 4 + hq / 2) + 8 * (hq & 1);
+    const uint32_t v_at = lds_address(s_v) + x * KB + 16 * v_place(x, hq);
+    auto load_k = [&](int page) {
+        const uint8_t *p = a.c.k + (int64_t)page * HALF;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-#pragma unroll
-            for (int s = 0; s < WIDE; ++s) r.k16[t][s] = *reinterpret_cast<const uint4 *>(p + 4 * t * D + 64 * s + 16 * hq);
-            if (ODD) r.k8[t][0] = *reinterpret_cast<const uint2 *>(p + 4 * t * D + 64 * WIDE + 8 * hq);
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = 64 * i + lane, token = at / (D / 16);
+            load_lds(p + token * D + 16 * k_place<D, true>(token, at % (D / 16)), s_k + 1024 * i);
         }
-        r.scales = *reinterpret_cast<const f32x2 *>(a.c.scales + (int64_t)page * 2);
     };
-    auto load_v = [&](KvBlock<D> &r, int page) {
-        const uint8_t *p = a.c.v + (int64_t)page * (KB * D) + x * KB + 16 * hq;
+    auto load_v = [&](int page) {
+        const uint8_t *p = a.c.v + (int64_t)page * HALF;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) r.v[i] = *reinterpret_cast<const uint4 *>(p + i * 16 * KB);
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = 64 * i + lane, d = at / 4;
+            load_lds(p + d * KB + 16 * v_place(d, at % 4), s_v + 1024 * i);
+        }
     };
 
     // logits of a block become weights: z in, p out, maximum and sum kept
@@ -517,85 +621,93 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
         return (typename T::x8){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
     };
 
-    KvBlock<D> r;
-    int j = 0, page = -1;
+    look(0);
     bool open = false;
-    int u = from + wave;
-    if (u < to) {
-        item(u, j, page, open);
-        page = __builtin_amdgcn_readfirstlane(page);
-        if (page >= 0) {
-            load_k(r, page);
-            load_v(r, page);
-        }
+    int page = __builtin_amdgcn_readlane(ps, 0);
+    if (many > 0 && page >= 0) {
+        load_k(page);
+        load_v(page);
     }
-    while (u < to) {
-        const int un = u + 4;
-        int jn = 0, pn = -1;
-        bool on = false;
-        if (un < to) item(un, jn, pn, on);
-        pn = __builtin_amdgcn_readfirstlane(pn);
-        f32x4 s[4];
+    for (int u = 0; u < many; ++u) {
+        const int j = __builtin_amdgcn_readlane(js, u & 63);
+        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[0]), u & 63)) * a.scale2;
+        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[1]), u & 63)) * T::VHALF;
+        if ((u & 63) == 63) look(u + 1);
+        const int pn = u + 1 < many ? __builtin_amdgcn_readlane(ps, (u + 1) & 63) : -1;
         if (page >= 0) {
-            const float ks = r.scales[0], half = r.scales[1] * T::VHALF;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < WIDE; ++i) {
-                    s[t] = T::mfma(bring8<T>(r.k16[t][i].x, r.k16[t][i].y, 1.f), q[2 * i], s[t]);
-                    s[t] = T::mfma(bring8<T>(r.k16[t][i].z, r.k16[t][i].w, 1.f), q[2 * i + 1], s[t]);
-                }
-                if (ODD) s[t] = T::mfma(bring8<T>(r.k8[t][0].x, r.k8[t][0].y, 1.f), q[KS - 1], s[t]);
-            }
-            if (pn >= 0) load_k(r, pn);
-            softmax(s, ks * a.scale2, j, (j + 1) * KB <= least);
-            const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
-#pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                o[i] = T::mfma(bring8<T>(r.v[i].x, r.v[i].y, half), p0, o[i]);
-                o[i] = T::mfma(bring8<T>(r.v[i].z, r.v[i].w, half), p1, o[i]);
-            }
-            if (pn >= 0) load_v(r, pn);
-        } else {
-            if (open) {
-                const int64_t tail = kv_tail(a.c, bh, b, nb, D);
-                const uint16_t *tk = a.c.tail_k + tail, *tv = a.c.tail_v + tail;
+            // on their way: this block's keys, then its values
+            wait_loads(LOADS);
+            f32x4 s[4];
+            {
+                KvKeys<D> k;
+                read_k<D>(k_at, k_more, k);
+                if (pn >= 0) load_k(pn);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
-                        s[t] = T::mfma(*reinterpret_cast<const typename T::x8 *>(tk + (kt + 4 * t) * D + d), q[ks], s[t]);
+                    for (int i = 0; i < WIDE; ++i) {
+                        s[t] = T::mfma(bring8<T>(k.wide[t][i].x, k.wide[t][i].y, 1.f), q[2 * i], s[t]);
+                        s[t] = T::mfma(bring8<T>(k.wide[t][i].z, k.wide[t][i].w, 1.f), q[2 * i + 1], s[t]);
                     }
+                    if (ODD) s[t] = T::mfma(bring8<T>(k.odd[t].x, k.odd[t].y, 1.f), q[KS - 1], s[t]);
                 }
-                softmax(s, a.scale2, j, false);
-                const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
-                // what no token has written yet may be anything: its values count as zero
-                const int held = len - nb * KB - 16 * hq;
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (i * 16 + x) * KB + 16 * hq + 8 * e);
-#pragma unroll
-                        for (int y = 0; y < 8; ++y) v[y] = 8 * e + y < held ? v[y] * (decltype(v[0] + v[0]))T::VHALF : 0;
-                        o[i] = T::mfma(v, e ? p1 : p0, o[i]);
-                    }
-                }
-            } else if (MASS && j >= 0 && j <= a.c.blocks && hq == 0 && valid) {
-                a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = -INFINITY;
             }
+            softmax(s, ks, j, (j + 1) * KB <= least);
+            const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+            // this block's values, then the next one's keys
+            if (pn >= 0)
+                wait_loads(LOADS);
+            else
+                wait_loads(0);
+            u32x4 v[DT];
+            read_v<DT>(v_at, v);
+            if (pn >= 0) load_v(pn);
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                o[i] = T::mfma(bring8<T>(v[i].x, v[i].y, vs), p0, o[i]);
+                o[i] = T::mfma(bring8<T>(v[i].z, v[i].w, vs), p1, o[i]);
+            }
+        } else {
+            if (page == -2)
+                open = true;
+            else if (MASS && hq == 0 && valid)
+                a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = -INFINITY;
             if (pn >= 0) {
-                load_k(r, pn);
-                load_v(r, pn);
+                load_k(pn);
+                load_v(pn);
             }
         }
-        u = un;
-        j = jn;
         page = pn;
-        open = on;
+    }
+    if (open) {  // the last block of the wave that has it
+        const int64_t tail = kv_tail(a.c, bh, b, nb, D);
+        const uint16_t *tk = a.c.tail_k + tail, *tv = a.c.tail_v + tail;
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int d = ks < 2 * WIDE ? 64 * (ks / 2) + 16 * hq + 8 * (ks % 2) : 64 * WIDE + 8 * hq;
+                s[t] = T::mfma(*reinterpret_cast<const typename T::x8 *>(tk + (kt + 4 * t) * D + d), q[ks], s[t]);
+            }
+        }
+        softmax(s, a.scale2, nb, false);
+        const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+        // what no token has written yet may be anything: its values count as zero
+        const int held = len - nb * KB - 16 * hq;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            __builtin_amdgcn_sched_barrier(0);  // few of these loads at once: two waves' registers have to fit
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (i * 16 + x) * KB + 16 * hq + 8 * e);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) v[y] = 8 * e + y < held ? v[y] * (decltype(v[0] + v[0]))T::VHALF : 0;
+                o[i] = T::mfma(v, e ? p1 : p0, o[i]);
+            }
+        }
     }
 
     // the four waves' results into one
@@ -606,6 +718,19 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
+    if constexpr (SOLO) {
+        if (!valid) return;
+        const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg;
+        const float f = l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const typename T::x2 p0 = T::narrow(o[i][0] * f, o[i][1] * f), p1 = T::narrow(o[i][2] * f, o[i][3] * f);
+            *reinterpret_cast<uint2 *>(a.out + at * D + 16 * i + 4 * hq) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+        }
+        if (a.lse && hq == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        return;
+    }
+    __syncthreads();  // no wave reads its block any more
     if (hq == 0) {
         s_ml[wave][x][0] = m;
         s_ml[wave][x][1] = l;
