@@ -201,6 +201,13 @@ def load_library():
     return lib
 
 
+def _current_stream(gpu: int) -> int:
+    """torch's current stream on that GPU, as a number."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # current_stream() without the object around it
+    return raw(gpu) if raw is not None else torch.cuda.current_stream(gpu).cuda_stream
+
+
 def _host(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(ctypes.c_void_p)
 
@@ -243,7 +250,12 @@ class KvCache:
         c = EtfKvCache(ETF_KV_BF16 if T == torch.bfloat16 else ETF_KV_FP16, B, H, D, table.shape[2], pages)
         for name in self.FIELDS:
             setattr(c, name, given[name].data_ptr())
+        self._set(c)
+
+    def _set(self, c):
         self._c, self._ref = c, ctypes.addressof(c)
+        self._gpu = self.device.index if self.device.type == "cuda" else -1
+        self._sizes = {}    # workspace bytes by call
 
     def __getattr__(self, name):
         if name in KvCache.FIELDS:
@@ -271,10 +283,15 @@ class KvCache:
     def fork(self) -> "KvCache":
         """Another table, lens and evicted (uninitialised) over the same pages and open blocks, for Context.kv_evict to write."""
         import torch
-        t = dict(self._t)
+        new = KvCache.__new__(KvCache)
+        new.__dict__.update(self.__dict__)
+        new._t = dict(self._t)
+        c = EtfKvCache.from_buffer_copy(self._c)
         for name in ("table", "lens", "evicted"):
-            t[name] = torch.empty_like(t[name])
-        return KvCache(**t)
+            t = new._t[name] = torch.empty_like(self._t[name])
+            setattr(c, name, t.data_ptr())
+        new._set(c)
+        return new
 
 
 class Context:
@@ -674,14 +691,14 @@ class Context:
 
     # ---- attention over a cache in 8 bits
     def _kv_here(self, cache: KvCache):
-        if self._device is not None and (cache.device.type, cache.device.index) != ("cuda", self._device):
+        if cache._gpu != self._device and self._device is not None:
             raise ValueError("the cache is on %s, the context on GPU %d" % (cache.device, self._device))
 
     @staticmethod
     def _rows(t, cache: KvCache, heads: Optional[int], what: str):
         """(pointer, strides) of rows [B][n][heads][D]; dense ones need no strides."""
         if t.dim() != 4 or t.shape[0] != cache.batch or t.shape[3] != cache.head_dim or (heads is not None and t.shape[2] != heads) or \
-                t.dtype != cache.dtype or t.device != cache.device or t.shape[1] < 1:
+                t.dtype != cache.dtype or t.get_device() != cache._gpu or t.shape[1] < 1:
             raise ValueError("%s: expected a %s tensor [%d][n][%s][%d] on %s" % (what, cache.dtype, cache.batch, "heads" if heads is None else heads, cache.head_dim, cache.device))
         if t.is_contiguous():
             return t.data_ptr(), None
@@ -694,7 +711,7 @@ class Context:
     def _kv_dev(t, shape, dtype, cache: KvCache, what: str):
         if t is None:
             return None
-        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != cache.device:
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != cache._gpu:
             raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (what, dtype, list(shape), cache.device))
         return t.data_ptr()
 
@@ -702,10 +719,18 @@ class Context:
         """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
         import torch
         mine = self._stream or 0
-        if torch.cuda.current_stream(cache.device).cuda_stream == mine:
+        if _current_stream(cache._gpu) == mine:
             return torch.empty(shape, dtype=dtype, device=cache.device)
         with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=cache.device)):
             return torch.empty(shape, dtype=dtype, device=cache.device)
+
+    def _kv_scratch(self, cache: KvCache, call, *args):
+        key = (call,) + args
+        size = cache._sizes.get(key)
+        if size is None:
+            size = cache._sizes[key] = call(self, cache, *args) + 256
+        import torch
+        return self._kv_empty((size,), torch.uint8, cache)
 
     def kv_append(self, cache: KvCache, k, v, counts=None):
         """Writes new tokens k, v [B][n][H][D] after cache.lens; the caller then advances cache.lens."""
@@ -731,14 +756,16 @@ class Context:
         pl = self._kv_dev(lists, (B, n, cache.heads, w), torch.int32, cache, "lists")
         pc = self._kv_dev(counts, (B,), torch.int32, cache, "counts")
         if out is None:
-            out = self._kv_empty((B, n, heads_q, D), cache.dtype, cache)
-        po = self._kv_dev(out, (B, n, heads_q, D), cache.dtype, cache, "out")
+            out = self._kv_empty(q.shape, cache.dtype, cache)
+            po = out.data_ptr()
+        else:
+            po = self._kv_dev(out, q.shape, cache.dtype, cache, "out")
         pe = self._kv_dev(lse, (B, n, heads_q), torch.float32, cache, "lse")
         blocks = (B, cache.heads, cache.max_blocks)
         pi = self._kv_dev(mass_in, blocks, torch.float32, cache, "mass_in")
         pm = self._kv_dev(mass_out, blocks, torch.float32, cache, "mass_out")
         if ws is None:
-            ws = self._kv_empty((self.kv_attend_workspace_bytes(cache, n, heads_q, w, pm is not None) + 256,), torch.uint8, cache)
+            ws = self._kv_scratch(cache, Context.kv_attend_workspace_bytes, n, heads_q, w, pm is not None)
         pw, nw = self._ws(ws)
         self._ck(self._lib.etf_kv_attend(self._h, cache._ref, pq, sq, n, heads_q, D ** -0.5 if scale is None else scale, pc, pl, w, po, pe, pi, pm, pw, nw))
         return out
@@ -754,7 +781,7 @@ class Context:
         B, n, heads_q, D = q.shape
         pc = self._kv_dev(counts, (B,), torch.int32, cache, "counts")
         if ws is None:
-            ws = self._kv_empty((self.kv_select_workspace_bytes(cache, n, heads_q, w) + 256,), torch.uint8, cache)
+            ws = self._kv_scratch(cache, Context.kv_select_workspace_bytes, n, heads_q, w)
         if lists is None:
             lists = self._kv_empty((B, n, cache.heads, w), torch.int32, cache)
         pl = self._kv_dev(lists, (B, n, cache.heads, w), torch.int32, cache, "lists")
