@@ -248,9 +248,11 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
         return mass_out ? launch_attend<T, D, false, true>(ctx, a, p) : launch_attend<T, D, false, false>(ctx, a, p);
     });
     if (rc != ETF_OK || !mass_out) return rc;
-    const int64_t grid = (int64_t)cache->batch * cache->heads * cache->max_blocks;
+    int width = 1;
+    while (width < 256 && width < n * a.g) width *= 2;
+    const int64_t blocks = (int64_t)cache->batch * cache->heads * cache->max_blocks, grid = (blocks + 256 / width - 1) / (256 / width);
     ProfScope prof(ctx, ETF_K_KV);
-    hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, mass_in, mass_out);
+    hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, width, mass_in, mass_out);
     LAUNCH_CHECK(ctx, "k_kv_mass");
     return ETF_OK;
 }
@@ -337,17 +339,21 @@ extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float
     const KvView c = view_of(cache);
     const dim3 grid((unsigned)(cache->batch * cache->heads));
     hipStream_t st = (hipStream_t)ctx->stream;
+    const bool apart = lens_out != cache->lens && evicted_out != cache->evicted && lens_out != cache->evicted && evicted_out != cache->lens;
+    int32_t *lens = apart ? lens_out : nullptr;
     if (cache->max_blocks <= 256)
-        hipLaunchKernelGGL((k_kv_evict<1, 4>), grid, dim3(64), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+        hipLaunchKernelGGL((k_kv_evict<1, 4>), grid, dim3(64), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+    else if (cache->max_blocks <= 1024)
+        hipLaunchKernelGGL((k_kv_evict<4, 4>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
     else if (cache->max_blocks <= 4096)
-        hipLaunchKernelGGL((k_kv_evict<4, 16>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+        hipLaunchKernelGGL((k_kv_evict<4, 16>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
     else if (cache->max_blocks <= KV_EVICT_MOST)
-        hipLaunchKernelGGL((k_kv_evict<16, 16>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+        hipLaunchKernelGGL((k_kv_evict<16, 16>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
     else
-        hipLaunchKernelGGL((k_kv_evict<16, 0>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed);
+        hipLaunchKernelGGL((k_kv_evict<16, 0>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
     LAUNCH_CHECK(ctx, "k_kv_evict");
-    hipLaunchKernelGGL(k_kv_evict_lens, dim3((unsigned)((cache->batch + 63) / 64)), dim3(64), 0, (hipStream_t)ctx->stream, view_of(cache), budget, lens_out,
-                       evicted_out);
+    if (apart) return ETF_OK;
+    hipLaunchKernelGGL(k_kv_evict_lens, dim3((unsigned)((cache->batch + 63) / 64)), dim3(64), 0, st, c, budget, lens_out, evicted_out);
     LAUNCH_CHECK(ctx, "k_kv_evict_lens");
     return ETF_OK;
 }

@@ -157,6 +157,8 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     __shared__ __attribute__((aligned(16))) uint8_t s_k[KB * D];
     __shared__ float s_amax[2][4];
     __shared__ int s_bad[KB];
+    constexpr int BW = D / 4, BG = 256 / BW, BT = (KB + BG - 1) / BG;  // bounds: words of a row, groups of tokens, tokens of a group
+    __shared__ __attribute__((aligned(8))) int16_t s_edge[2][BG][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t bh = blockIdx.x / a.per;
     const int h = (int)(bh % a.c.heads), b = (int)(bh / a.c.heads), blk = blockIdx.x % a.per;
@@ -226,21 +228,44 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
                 const uint32_t *r = reinterpret_cast<const uint32_t *>(s_v + p / 4 * VROW + p % 4 * 16);
                 reinterpret_cast<uint4 *>(a.c.v + (int64_t)page * (KB * D))[p] = make_uint4(r[0], r[1], r[2], r[3]);
             }
-            if (tid < D) {
-                int lo = 0x7F, hi = -0x7F;
-                for (int t = 0; t < KB; ++t) {
+            // smallest and largest codes: four dimensions and a group of tokens to a thread, then the groups
+            if (tid < BW * BG) {
+                const int w = tid % BW, grp = tid / BW;
+                int lo[4] = {0x7F, 0x7F, 0x7F, 0x7F}, hi[4] = {-0x7F, -0x7F, -0x7F, -0x7F};
+                for (int t = grp * BT; t < min(KB, (grp + 1) * BT); ++t) {
                     if (s_bad[t]) continue;
-                    const int o = code_order(s_k[t * D + tid]);
-                    lo = min(lo, o);
-                    hi = max(hi, o);
+                    const uint32_t u = *reinterpret_cast<const uint32_t *>(s_k + t * D + 4 * w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int o = code_order(u >> (8 * i));
+                        lo[i] = min(lo[i], o);
+                        hi[i] = max(hi[i], o);
+                    }
                 }
-                if (lo > hi) lo = hi = 0;
-                a.c.bounds[((int64_t)page * 2) * D + tid] = code_of_order(lo);
-                a.c.bounds[((int64_t)page * 2 + 1) * D + tid] = code_of_order(hi);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s_edge[0][grp][4 * w + i] = (int16_t)lo[i];
+                    s_edge[1][grp][4 * w + i] = (int16_t)hi[i];
+                }
             }
             if (tid < 2) a.c.scales[(int64_t)page * 2 + tid] = ldexpf(1.f, tid ? ev : ek);
         }
         __syncthreads();
+        if (page >= 0 && tid < 2 * BW) {
+            const int e = tid / BW, d = tid % BW * 4;
+            uint32_t out = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int lo = 0x7F, hi = -0x7F;
+                for (int y = 0; y < BG; ++y) {
+                    lo = min(lo, (int)s_edge[0][y][d + i]);
+                    hi = max(hi, (int)s_edge[1][y][d + i]);
+                }
+                const int o = lo > hi ? 0 : e ? hi : lo;
+                out |= (uint32_t)code_of_order(o) << (8 * i);
+            }
+            *reinterpret_cast<uint32_t *>(a.c.bounds + ((int64_t)page * 2 + e) * D + d) = out;
+        }
     }
     if (blk > 0) return;
     // what is left over: tokens [from, left) of the open block
@@ -1077,28 +1102,31 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a)
 }
 
 // Weight of every block in this call, summed over the rows of a (sequence, head): 2^(block's logarithm - row's logarithm).
-// A workgroup to a block; sums in 64 bits, in an order that does not depend on the launch.
-__global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restrict__ row_lse, const float *__restrict__ block_lse, int rows,
+// `width` lanes to a block, a power of two: with few rows a workgroup has many blocks (4 rows of 16 x 8 x 128 blocks: 12.6 us with one
+// to a workgroup).  Sums in 64 bits, in an order that does not depend on the launch.
+__global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restrict__ row_lse, const float *__restrict__ block_lse, int rows, int width,
                                                  const float *mass_in, float *mass_out)
 {
     __shared__ double s_sum[4];
-    const int64_t bh = blockIdx.x / c.blocks;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x % c.blocks;
-    const int b = (int)(bh / c.heads), held = (kv_len(c, b) + KB - 1) / KB;
+    const int64_t at = (int64_t)blockIdx.x * (256 / width) + threadIdx.x / width, bh = at / c.blocks;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = threadIdx.x & (width - 1), j = (int)(at % c.blocks);
+    const bool there = bh < (int64_t)c.batch * c.heads;
     double sum = 0;
-    if (j < held)
-        for (int r = threadIdx.x; r < rows; r += 256) {
+    if (there && j < (kv_len(c, (int)(bh / c.heads)) + KB - 1) / KB)
+        for (int r = first; r < rows; r += width) {
             const float lr = row_lse[bh * rows + r];
             // a row that sees nothing adds nothing
             if (lr != -INFINITY) sum += (double)__builtin_amdgcn_exp2f(block_lse[(bh * (c.blocks + 1) + j) * rows + r] - lr);
         }
-    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) s_sum[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const float was = mass_in ? mass_in[bh * c.blocks + j] : 0.f;
-        mass_out[bh * c.blocks + j] = was + (float)(s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
+    for (int o = min(width, 64) / 2; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (width > 64) {
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        const int w0 = threadIdx.x / width * (width / 64);
+        sum = s_sum[w0] + s_sum[w0 + 1];
+        if (width == 256) sum += s_sum[2] + s_sum[3];
     }
+    if (there && first == 0) mass_out[at] = (mass_in ? mass_in[at] : 0.f) + (float)sum;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1248,8 +1276,9 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
 // ------------------------------------------------------------------------------------------------
 // The `w` largest of `n` keys that are not zero, ties to the lower index.  WAVES waves take one row together; a wave holds up to 64 KPT
 // consecutive keys in registers.  The w-th largest key is found by counting, with ballots, how many keys reach a number between two
-// bounds; where it would lie among evenly spread keys is tried first, and the walk ends once exactly w keys reach a
-// number: some eight counts for scores, two for a bit at most.  Rows longer than the registers read their keys again for every bit (KPT = 0).
+// bounds; where it would lie among evenly spread keys is tried first.  The walk ends once exactly w keys reach a number, or no more than 64
+// lie between the bounds (some four counts for scores, two for a bit at most): those are ranked against one another.  Rows longer
+// than the registers read their keys again for every count (KPT = 0).
 // ------------------------------------------------------------------------------------------------
 template <typename U, int WAVES, int KPT>
 struct Pick {
@@ -1276,7 +1305,17 @@ struct Pick {
     __device__ __forceinline__ int reach(U x, Key key, int (&s_sum)[2][WAVES], int turn) const
     {
         int c = 0;
-        if constexpr (KPT > 0) {
+        if constexpr (KPT >= 8) {  // a lane counts its own keys (those past the row are 0), then the lanes' counts are added bit by bit
+            static_assert(KPT % 4 == 0 && KPT < 32, "in groups of four, counts of five bits");
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < KPT; i += 4)
+                if (from + 64 * i < n)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) mine += keys[i + y] >= x;
+#pragma unroll
+            for (int y = 0; y < 5; ++y) c += __popcll(__ballot(mine >> y & 1)) << y;
+        } else if constexpr (KPT > 0) {
 #pragma unroll
             for (int i = 0; i < KPT; ++i)
                 if (from + 64 * i < n) c += __popcll(__ballot(keys[i] >= x));
@@ -1292,20 +1331,76 @@ struct Pick {
         return all;
     }
 
-    template <typename Key>
-    __device__ __forceinline__ void load(int n_, Key key)
+    // a row of n keys; key number i of this lane is the row's place(i)
+    __device__ __forceinline__ void row(int n_)
     {
         n = n_;
         span = KPT ? 64 * KPT : (n + 64 * WAVES - 1) / (64 * WAVES) * 64;
         from = wave() * span;
+    }
+    __device__ __forceinline__ int place(int i) const { return from + 64 * i + lane(); }
+    template <typename Key>
+    __device__ __forceinline__ void load(int n_, Key key)
+    {
+        row(n_);
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) {
-            const int j = from + 64 * i + lane();
-            keys[i] = KPT && j < n ? key(j) : 0;
-        }
+        for (int i = 0; i < KEYS; ++i) keys[i] = KPT && place(i) < n ? key(place(i)) : 0;
     }
 
-    // after load(); turn: the buffer of the row's last count
+    static __device__ __forceinline__ uint32_t of_lane(uint32_t x, int l) { return __builtin_amdgcn_readlane(x, l); }
+    static __device__ __forceinline__ uint64_t of_lane(uint64_t x, int l)
+    {
+        return (uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, l);
+    }
+
+    // The w-th largest of the up to 64 keys in [l, r), `many` of them
+    __device__ __forceinline__ void rank(U l, U r, int w, int many)
+    {
+        __shared__ U s_few[WAVES == 1 ? 4 : 1][64];
+        __shared__ int s_count;
+        U *few = s_few[WAVES == 1 ? threadIdx.x >> 6 : 0];
+        int c = 0;
+        uint64_t in[KEYS];
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            in[i] = __ballot(keys[i] >= l && keys[i] < r);
+            c += __popcll(in[i]);
+        }
+        if (WAVES > 1) {
+            if (threadIdx.x == 0) s_count = 0;
+            __syncthreads();
+            int at = 0;
+            if (c > 0 && lane() == 0) at = atomicAdd(&s_count, c);
+            c = __builtin_amdgcn_readfirstlane(at);
+        } else {
+            c = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int at = c + __popcll(in[i] & ((1ull << lane()) - 1));
+            if (in[i] >> lane() & 1) few[at & 63] = keys[i];
+            c += __popcll(in[i]);
+        }
+        if (WAVES > 1) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        const U own = lane() < many ? few[lane()] : 0;
+        int above = 0, same = 0;
+        for (int z = 0; z < many; ++z) {
+            const U other = of_lane(own, z);
+            above += other > own;
+            same += other == own;
+        }
+        const uint64_t hit = __ballot(lane() < many && above < w && above + same >= w);
+        const int at = __ffsll((unsigned long long)hit) - 1;
+        cut = of_lane(own, at);
+        ties = w - __builtin_amdgcn_readlane(above, at);
+    }
+
+    // after the keys are there; turn: the buffer of the row's last count
     template <typename Key>
     __device__ __forceinline__ void find(int w, Key key, int (&s_sum)[2][WAVES], int &turn)
     {
@@ -1351,6 +1446,12 @@ struct Pick {
         }
         ++r;
         for (int turns = 0; r - l > 1; ++turns) {
+            if constexpr (KPT > 0) {
+                if (cl - cr <= 64) {
+                    rank(l, r, w - cr, cl - cr);
+                    return;
+                }
+            }
             // where the w-th key would lie if they were spread evenly, and the middle, in turn
             const U gap = r - l;
             U step = gap / 2;
@@ -1515,8 +1616,21 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
     const uint16_t *q = a.q + b * a.qs[0] + i * a.qs[1] + (int64_t)h * a.g * a.qs[2];
     int got = -1;
     Pick<uint32_t, WAVES, KPT> lower, upper;
-    lower.load(whole, low);
-    upper.load(whole, high);
+    lower.row(whole);
+    upper.row(whole);
+    float widest = 0.f;  // interval of those that are not forced
+    if constexpr (KPT > 0) {
+        uint64_t raw[KPT];  // all on their way together
+#pragma unroll
+        for (int y = 0; y < KPT; ++y) raw[y] = scores[min(lower.place(y), a.c.blocks - 1)];
+#pragma unroll
+        for (int y = 0; y < KPT; ++y) {
+            const int j = lower.place(y);
+            lower.keys[y] = j < whole ? low_of(j, raw[y]) : 0;
+            upper.keys[y] = j < whole ? high_of(j, raw[y]) : 0;
+            if (j < whole && !forced(j)) widest = fmaxf(widest, __uint_as_float((uint32_t)(raw[y] >> 32)));
+        }
+    }
     lower.find(a.w, low, s_sum, turn);
     // w blocks reach `least` with their lower ends: one whose upper end does not cannot be chosen
     const uint32_t least = lower.ties ? lower.cut : lower.cut + 1;
@@ -1531,12 +1645,6 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
         __shared__ uint64_t s_open[ROWS * WAVES][64];
         __shared__ int s_found[2][WAVES];
         int *list = reinterpret_cast<int *>(s_open[threadIdx.x >> 6]);  // the wave's open blocks
-        float widest = 0.f;
-#pragma unroll
-        for (int y = 0; y < KPT; ++y) {
-            const int j = lower.from + 64 * y + lane;
-            if (j < whole && !forced(j)) widest = fmaxf(widest, __uint_as_float((uint32_t)(scores[j] >> 32)));
-        }
         for (int o = 32; o; o >>= 1) widest = fmaxf(widest, __shfl_xor(widest, o));
         if (WAVES > 1) {
             if (lane == 0) s_widest[wave] = widest;
@@ -1587,15 +1695,19 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
                 need -= s_found[0][y];
                 fits = fits && s_found[1][y] <= 64;
             }
-            if (fits)
-                for (int y = 0; y < WAVES; ++y)
-                    for (int z = 0; z < s_found[1][y]; ++z) {
-                        const uint64_t other = s_open[y][z];
+            if (fits && opens > 0)
+                for (int y = 0; y < WAVES; ++y) {
+                    const int found = __builtin_amdgcn_readfirstlane(s_found[1][y]);
+                    if (found == 0) continue;
+                    const uint64_t others = s_open[y][lane];
+                    for (int z = 0; z < found; ++z) {
+                        const uint64_t other = Pick<uint64_t, WAVES, KPT>::of_lane(others, z);
                         ahead += other > own || (other == own && (y < wave || (y == wave && z < lane)));
                     }
+                }
         } else if (fits) {
             for (int z = 0; z < opens; ++z) {
-                const uint64_t other = __shfl(own, z);
+                const uint64_t other = Pick<uint64_t, WAVES, KPT>::of_lane(own, z);
                 ahead += other > own || (other == own && z < lane);
             }
         }
@@ -1650,14 +1762,14 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // Eviction: of every (sequence, head) with more than `budget` blocks the first `sink`, the last `recent` and those of
-// the others with the largest weight stay, in their order.  The lengths change in a launch of their own (k_kv_evict_lens): every
-// workgroup here reads them, and they may be changed in place.
+// the others with the largest weight stay, in their order.  Lengths that are changed in place change in a launch of their own
+// (k_kv_evict_lens), since every workgroup here reads them; into other arrays (lens_out not null) they are written here.
 // ------------------------------------------------------------------------------------------------
 // Everything is read before anything is written, since the outputs may be the inputs; with more blocks than the registers hold a launch
 // of one workgroup per row has to write apart from what it reads (KPT = 0: `table_out` and `mass_out` are not the inputs).
 template <int WAVES, int KPT>
 __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *mass, int budget, int sink, int recent, int32_t *table_out, float *mass_out,
-                                                         int32_t *freed)
+                                                         int32_t *freed, int32_t *lens_out, int32_t *evicted_out)
 {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / c.heads), tid = threadIdx.x;
@@ -1668,6 +1780,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
     mass_out += bh * c.blocks;
     freed += bh * c.blocks;
     const float open = nb < c.blocks ? mass[nb] : 0.f;  // the open block's weight moves along
+    if (lens_out && bh % c.heads == 0 && tid == 0) {
+        const int len = kv_len(c, b), gone = max(0, len / KB - budget);
+        lens_out[b] = len - gone * KB;
+        evicted_out[b] = c.evicted[b] + gone;
+    }
     auto key = [&](int j) -> uint64_t {
         if (j < sink || j >= nb - recent) return ~0ull;
         return key_of((double)mass[j]);
@@ -1675,21 +1792,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
     __shared__ int s_sum[2][WAVES];
     int turn = 0;
     Pick<uint64_t, WAVES, KPT> pick;
-    pick.load(nb, key);
-    pick.find(budget, key, s_sum, turn);
     int32_t page[KPT ? KPT : 1];
     float weight[KPT ? KPT : 1];
-    if (KPT) {
+    pick.row(nb);
+    if constexpr (KPT > 0) {  // all on their way together
 #pragma unroll
         for (int i = 0; i < KPT; ++i) {
-            const int j = pick.from + 64 * i + pick.lane();
-            if (j < nb) {
-                page[i] = table[j];
-                weight[i] = mass[j];
-            }
+            const int j = min(pick.place(i), c.blocks - 1);
+            page[i] = table[j];
+            weight[i] = mass[j];
         }
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int j = pick.place(i);
+            pick.keys[i] = j >= nb ? 0 : j < sink || j >= nb - recent ? ~0ull : key_of((double)weight[i]);
+        }
     }
+    pick.find(budget, key, s_sum, turn);
+    if (KPT) __syncthreads();
     pick.walk(key, [&](int j, int place, bool take) {
         int32_t p;
         float w;
@@ -1698,7 +1818,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
             w = 0.f;
 #pragma unroll
             for (int i = 0; i < KPT; ++i)
-                if (j - pick.lane() - pick.from == 64 * i) {
+                if (j == pick.place(i)) {
                     p = page[i];
                     w = weight[i];
                 }
