@@ -1274,6 +1274,28 @@ __global__ __launch_bounds__(256) void k_kv_score(KvSelectArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------
+// The largest of a wave's numbers, in all lanes
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_from(uint32_t x)
+{
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max_from<0x111, 0xf>(x);  // one, two, four and eight lanes up within rows of 16
+    x = max_from<0x112, 0xf>(x);
+    x = max_from<0x114, 0xf>(x);
+    x = max_from<0x118, 0xf>(x);
+    x = max_from<0x142, 0xa>(x);  // a row's last lane into the next row, of the first half into the second
+    x = max_from<0x143, 0xc>(x);
+    return __builtin_amdgcn_readlane(x, 63);
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t x)
+{
+    const uint32_t top = wave_max((uint32_t)(x >> 32));
+    return (uint64_t)top << 32 | wave_max(x >> 32 == top ? (uint32_t)x : 0u);
+}
+
 // The `w` largest of `n` keys that are not zero, ties to the lower index.  WAVES waves take one row together; a wave holds up to 64 KPT
 // consecutive keys in registers.  The w-th largest key is found by counting, with ballots, how many keys reach a number between two
 // bounds; where it would lie among evenly spread keys is tried first.  The walk ends once exactly w keys reach a number, or no more than 64
@@ -1328,7 +1350,7 @@ struct Pick {
         int all = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) all += s_sum[turn][i];
-        return all;
+        return __builtin_amdgcn_readfirstlane(all);
     }
 
     // a row of n keys; key number i of this lane is the row's place(i)
@@ -1427,11 +1449,8 @@ struct Pick {
         } else {
             for (int k = 0; k < span && from + k < n; k += 64) ends(at(k / 64, key));
         }
-        for (int o = 32; o; o >>= 1) {
-            const U x = __shfl_xor(l, o), y = __shfl_xor(r, o);
-            l = x < l ? x : l;
-            r = y > r ? y : r;
-        }
+        l = ~wave_max((U)~l);
+        r = wave_max(r);
         if (WAVES > 1) {
             __shared__ U s_ends[2][WAVES];
             if (lane() == 0) {
@@ -1443,6 +1462,8 @@ struct Pick {
                 l = s_ends[0][i] < l ? s_ends[0][i] : l;
                 r = s_ends[1][i] > r ? s_ends[1][i] : r;
             }
+            l = of_lane(l, 0);
+            r = of_lane(r, 0);
         }
         ++r;
         for (int turns = 0; r - l > 1; ++turns) {
@@ -1457,7 +1478,7 @@ struct Pick {
             U step = gap / 2;
             if (turns % 2 == 0) step = (U)((float)gap * ((cl - w + 0.5f) / (float)(cl - cr)));
             step = step < 1 ? 1 : step > gap - 1 ? gap - 1 : step;
-            const U x = l + step;
+            const U x = of_lane((U)(l + step), 0);
             const int c = reach(x, key, s_sum, turn ^= 1);
             if (c == w) {
                 cut = x - 1;
@@ -1476,8 +1497,9 @@ struct Pick {
         ties = w - cr;
     }
 
-    // Calls put(j, place, chosen) for every j < n, place = how many of its kind come before it; returns the number of chosen ones.
-    template <typename Key, typename Put>
+    // Calls put(j, place, chosen) for every j < n (ALL) or every chosen one, place = how many of its kind come before it; returns the
+    // number of chosen ones.
+    template <bool ALL, typename Key, typename Put>
     __device__ __forceinline__ int walk(Key key, Put put) const
     {
         __shared__ int s_kind[2][WAVES];
@@ -1518,6 +1540,7 @@ struct Pick {
         auto round = [&](int k, U v) {
             const int j = from + k + lane();
             const uint64_t bo = __ballot(v > cut), bs = __ballot(v != 0 && v == cut);
+            if (!ALL && (bo | bs) == 0) return;
             const int os = same + __popcll(bs & below);
             const bool take = v > cut || (v != 0 && v == cut && os < ties);
             const int place = over + __popcll(bo & below) + min(os, ties);
@@ -1591,7 +1614,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
     const int H = a.c.heads, b = (int)(row / H / a.n), i = (int)(row / H % a.n), h = (int)(row % H);
     if (b >= a.c.batch) return;
     const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
-    const int whole = i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0;
+    const int whole = __builtin_amdgcn_readfirstlane(i < count ? min(max(0, len - count + i + 1) / KB, a.c.blocks) : 0);
     __shared__ int s_sum[2][WAVES];
     int turn = 0;
     uint64_t *scores = a.scores + row * a.c.blocks;
@@ -1636,7 +1659,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
     const uint32_t least = lower.ties ? lower.cut : lower.cut + 1;
     if (upper.reach(least, high, s_sum, turn ^= 1) <= a.w) {
         upper.cut = least - 1;
-        got = upper.walk(high, put);
+        got = upper.template walk<false>(high, put);
     } else if constexpr (KPT > 0) {
         // No more than w blocks have a lower end above `least` (or w have one from there on), so no more than w an upper end that lies
         // by the widest interval above it: a block whose lower end does is chosen.  The few between, up to 64 of a wave, are
@@ -1645,7 +1668,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
         __shared__ uint64_t s_open[ROWS * WAVES][64];
         __shared__ int s_found[2][WAVES];
         int *list = reinterpret_cast<int *>(s_open[threadIdx.x >> 6]);  // the wave's open blocks
-        for (int o = 32; o; o >>= 1) widest = fmaxf(widest, __shfl_xor(widest, o));
+        widest = __uint_as_float(wave_max(__float_as_uint(widest)));  // not negative: ordered like its bits
         if (WAVES > 1) {
             if (lane == 0) s_widest[wave] = widest;
             __syncthreads();
@@ -1723,7 +1746,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
             }
             upper.cut = 0;
             upper.ties = 0;
-            got = upper.walk(high, put);
+            got = upper.template walk<false>(high, put);
         }
     }
     if (got < 0) {  // many blocks alike: the exact scores of all that may be chosen, in the place of their bounds
@@ -1755,7 +1778,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
         Pick<uint64_t, WAVES, KPT> last;
         last.load(whole, key);
         last.find(a.w, key, s_sum, turn);
-        got = last.walk(key, put);
+        got = last.template walk<false>(key, put);
     }
     for (int j = got + threadIdx.x % (64 * WAVES); j < a.w; j += 64 * WAVES) out[j] = -1;
 }
@@ -1773,7 +1796,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
 {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / c.heads), tid = threadIdx.x;
-    const int nb = min(kv_len(c, b) / KB, c.blocks), stay = min(nb, budget);
+    const int nb = __builtin_amdgcn_readfirstlane(min(kv_len(c, b) / KB, c.blocks)), stay = min(nb, budget);
     const int32_t *table = c.table + bh * c.blocks;
     mass += bh * c.blocks;
     table_out += bh * c.blocks;
@@ -1810,7 +1833,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
     }
     pick.find(budget, key, s_sum, turn);
     if (KPT) __syncthreads();
-    pick.walk(key, [&](int j, int place, bool take) {
+    pick.template walk<true>(key, [&](int j, int place, bool take) {
         int32_t p;
         float w;
         if (KPT) {
