@@ -97,7 +97,8 @@ struct AttendPlan {
     bool many = false;  // tiles of 128 rows instead of 16
     bool solo = false;  // listed blocks: a wave to a unit
     int tiles = 0, splits = 1, rows = 16;
-    int64_t units = 0, target = 0, grid = 0, o_ml = 0, o_row = 0, o_block = 0, total = 0;
+    bool split = false;  // whole caches: into ranges
+    int64_t units = 0, grid = 0, o_ml = 0, o_plan = 0, o_row = 0, o_block = 0, total = 0;
 };
 
 AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool mass)
@@ -109,7 +110,7 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         p.tiles = (g + 15) / 16;
         p.units = (int64_t)c->batch * n * c->heads * p.tiles;
         // enough workgroups for the card, none with less than a block to a wave
-        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 768 / std::max<int64_t>(1, p.units)));
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 512 / std::max<int64_t>(1, p.units)));
         p.solo = p.units >= 2048;
         p.grid = p.solo ? (p.units + 3) / 4 : p.units * p.splits;
     } else {
@@ -117,14 +118,17 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         p.rows = p.many ? 128 : 16;
         p.tiles = (int)((rows + p.rows - 1) / p.rows);
         p.units = (int64_t)p.tiles * c->heads;
-        // a card full of workgroups from the tiles alone needs no ranges
-        p.target = p.many ? (c->batch * p.units >= 1024 ? 0 : 512) : 1024;
-        p.grid = p.target + c->batch * p.units;
+        // up to KV_ROUNDS rounds of workgroups (kv_plan) and one for each unit of a sequence; a card full of workgroups from the tiles of prompts alone
+        // needs no ranges
+        const int64_t units = c->batch * p.units;
+        p.split = !p.many || units < 1024;
+        p.grid = (p.split ? KV_ROUNDS * KV_ROUND : 0) + units;
     }
-    const bool parts = w > 0 ? p.splits > 1 : p.target > 0;
+    const bool parts = w > 0 ? p.splits > 1 : p.split;
     const int64_t slots = parts ? p.grid * p.rows : 0;
     p.o_ml = al256(slots * c->head_dim * 4);
-    p.o_row = p.o_ml + al256(slots * 2 * 4);
+    p.o_plan = p.o_ml + al256(slots * 2 * 4);
+    p.o_row = p.o_plan + (p.split ? al256((int64_t)c->batch * 16) : 0);
     const int64_t all_rows = mass ? (int64_t)c->batch * c->heads * rows : 0;
     p.o_block = p.o_row + al256(all_rows * 4);
     p.total = std::max<int64_t>(256, p.o_block + al256(all_rows * (c->max_blocks + 1) * 4));
@@ -140,7 +144,7 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
         if (p.many) {
             hipLaunchKernelGGL((k_kv_tile<T, D, MASS>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
             LAUNCH_CHECK(ctx, "k_kv_tile");
-            if (p.target > 0) {
+            if (p.split) {
                 hipLaunchKernelGGL((k_kv_join<T, D, 128, false, MASS>), dim3((unsigned)(a.c.batch * p.units * 16)), dim3(256), 0, st, a);
                 LAUNCH_CHECK(ctx, "k_kv_join");
             }
@@ -156,7 +160,7 @@ int launch_attend(etf_ctx *ctx, const KvAttendArgs &a, const AttendPlan &p)
     }
     hipLaunchKernelGGL((k_kv_attend<T, D, LIST, MASS, false>), dim3((unsigned)p.grid), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_attend");
-    if (LIST ? p.splits > 1 : p.target > 0) {
+    if (LIST ? p.splits > 1 : p.split) {
         const int64_t units = LIST ? p.units : a.c.batch * p.units;
         hipLaunchKernelGGL((k_kv_join<T, D, 16, LIST, MASS>), dim3((unsigned)units * 2), dim3(256), 0, st, a);
         LAUNCH_CHECK(ctx, "k_kv_join");
@@ -230,6 +234,7 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
     a.lse = lse;
     a.part_o = (float *)base;
     a.part_ml = (float *)(base + p.o_ml);
+    a.plan = (int4 *)(base + p.o_plan);
     a.row_lse = (float *)(base + p.o_row);
     a.block_lse = (float *)(base + p.o_block);
     a.scale2 = scale * 1.4426950408889634f;
@@ -239,7 +244,7 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
     a.splits = p.splits;
     a.tiles = p.tiles;
     a.units = p.units;
-    a.target = p.target;
+    a.split = p.split;
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     rc = with_shape(cache, [&](auto t, auto dim) {
         using T = decltype(t);

@@ -316,57 +316,107 @@ struct KvAttendArgs {
     uint16_t *out;
     float *lse;
     float *part_o, *part_ml;  // partial results of ranges: [slot][rows of a tile][D], [slot][rows of a tile][2]
+    int4 *plan;               // [b]: what k_kv_join needs of the sequence's ranges
     float *row_lse, *block_lse;  // logarithms (base 2) for the blocks' weights: [b][h][row], [b][h][blocks + 1][row]
     float scale2;  // softmax scale times log2 e
     int n, g, w, splits;
     int tiles;        // row tiles of a (sequence, head): of all tokens, or of one token where blocks are listed
     int64_t units;    // listed: (sequence, token, tile, head) units
-    int64_t target;   // workgroups that a whole-cache call aims at
+    bool split;       // whole caches: into ranges
 };
 
-constexpr int KV_LEAST = 4;  // blocks of a range, one to a wave
+constexpr int KV_LEAST = 4;    // blocks of a range, one to a wave
+constexpr int KV_ROUND = 512;  // workgroups that the card holds at once
+constexpr int KV_ROUNDS = 3;   // most rounds of them that ranges are made for
 
+// A sequence's workgroups: `live` tiles of `tiles` have rows that are no padding; first the ranges of those, heads innermost, then one to
+// each (tile, head) of padding.
 struct KvRange {
-    int b, splits, per;  // sequence; ranges of its blocks; blocks of a range
-    int64_t first;       // number of its first workgroup
+    int b, live, splits, per;  // sequence; its tiles; ranges of its blocks; blocks of a range
+    int first;                 // number of its first workgroup
 };
 
-// Workgroup numbers of a call over whole caches: every sequence gets ranges of `per` blocks for each of its `units` (tiles of rows
-// times heads), `per` from the blocks of all sequences, so that the lengths on the device decide the split and long
-// sequences get more workgroups.  find >= 0: the sequence that workgroup `find` works for (b = batch: none); else sequence b's.
-// Every lane of the wave calls it.
-__device__ __forceinline__ KvRange kv_plan(const KvView &c, int units, int64_t target, int64_t find, int b)
+// Sums over the lanes up to each one
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int x)
 {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int i = lane; i < c.batch; i += 64) total += (kv_len(c, i) + KB - 1) / KB;
-    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int sum_upto(int x)
+{
+    x = add_from<0x111, 0xf>(x);  // one, two, four and eight lanes up within rows of 16
+    x = add_from<0x112, 0xf>(x);
+    x = add_from<0x114, 0xf>(x);
+    x = add_from<0x118, 0xf>(x);
+    x = add_from<0x142, 0xa>(x);  // a row's last lane into the next row, of the first half into the second
+    return add_from<0x143, 0xc>(x);
+}
+
+// Workgroup numbers of a call over whole caches: every sequence gets ranges of up to `per` blocks for each of its live tiles of ROWS rows and
+// heads, of one length within the sequence, and `per` comes from the blocks of all sequences, so that the lengths on the device decide
+// the split and long sequences get more workgroups.  Of the splits into one to three rounds of workgroups the one is taken whose rounds times
+// blocks of a range, with four more for a range's start and its join, are the least.  The sequence that workgroup `find` works for
+// (b = batch: none); its first workgroup leaves the ranges for k_kv_join (planning there again: 29 us instead of 15 for pieces of three
+// prompts).  Every lane of the wave calls it.
+template <int ROWS>
+__device__ __forceinline__ KvRange kv_plan(const KvAttendArgs &a, int find)
+{
+    constexpr int LEAST = ROWS == 16 ? KV_LEAST : 1;  // the waves of a tile of 128 rows take the same blocks
+    const int lane = threadIdx.x & 63, batch = a.c.batch, H = a.c.heads;
+    auto blocks_of = [&](int i) { return i < batch ? (kv_len(a.c, i) + KB - 1) / KB : 0; };
+    auto live_of = [&](int i) { return i < batch ? (kv_count(a.counts, i, a.n) * a.g + ROWS - 1) / ROWS : 0; };
     KvRange r;
-    r.per = target > 0 ? (int)max((int64_t)KV_LEAST, (total * units + target - 1) / target) : 1 << 30;  // 0: no splits
-    int64_t base = 0;
-    for (int i0 = 0; i0 < c.batch; i0 += 64) {
-        const int i = i0 + lane;
-        const int s = i < c.batch ? max(1, ((kv_len(c, i) + KB - 1) / KB + r.per - 1) / r.per) : 0;
-        int64_t upto = (int64_t)s * units;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t x = __shfl_up(upto, o);
-            if (lane >= o) upto += x;
+    r.per = 1 << 30;  // no splits
+    if (a.split) {
+        const int blocks0 = blocks_of(lane), live0 = live_of(lane);  // of the first 64 sequences, as a rule all
+        int units = 0;
+        double total = 0;  // whole numbers below 2^53
+        for (int i0 = 0; i0 < batch; i0 += 64) {
+            const int blocks = i0 ? blocks_of(i0 + lane) : blocks0, live = i0 ? live_of(i0 + lane) : live0;
+            units += __builtin_amdgcn_readlane(sum_upto(live), 63) * H;
+            const uint64_t both = (uint64_t)blocks * live;  // below 2^48: added up in two halves
+            total += (16777216.0 * __builtin_amdgcn_readlane(sum_upto((int)(both >> 24)), 63) + __builtin_amdgcn_readlane(sum_upto((int)(both & 0xFFFFFF)), 63)) * H;
         }
-        upto += base;
-        const uint64_t hit = __ballot(i < c.batch && (find >= 0 ? upto > find : i == b));
+        int64_t least = INT64_MAX;
+        for (int rounds = 1; rounds <= KV_ROUNDS; ++rounds) {
+            // ranges come to no more than the divisor and one for each unit
+            const int room = rounds * KV_ROUND - units;
+            if (room <= 0 && rounds < KV_ROUNDS) continue;
+            const int per = max(LEAST, (int)min(1073741824.0, ceil(total / (room > 0 ? room : 2 * KV_ROUND))));
+            int many = 0;
+            for (int i0 = 0; i0 < batch; i0 += 64) {
+                const int blocks = i0 ? blocks_of(i0 + lane) : blocks0, live = i0 ? live_of(i0 + lane) : live0;
+                many += __builtin_amdgcn_readlane(sum_upto(max(1, (blocks + per - 1) / per) * live), 63) * H;
+            }
+            const int64_t cost = (int64_t)((many + KV_ROUND - 1) / KV_ROUND) * (per + 4);
+            if (cost < least) {
+                least = cost;
+                r.per = per;
+            }
+            if (per == LEAST) break;
+        }
+        r.per = __builtin_amdgcn_readfirstlane(r.per);
+    }
+    int base = 0;
+    for (int i0 = 0; i0 < batch; i0 += 64) {
+        const int i = i0 + lane, blocks = blocks_of(i), live = live_of(i), s = i < batch ? max(1, (blocks + r.per - 1) / r.per) : 0;
+        const int upto = base + sum_upto(i < batch ? (s - 1) * live + a.tiles : 0) * H;
+        const uint64_t hit = __ballot(i < batch && upto > find);
         if (hit) {
             const int l = __ffsll((unsigned long long)hit) - 1;
             r.b = i0 + l;
-            r.splits = __builtin_amdgcn_readfirstlane(__shfl(s, l));
-            const int64_t end = __shfl(upto, l);
-            r.first = end - (int64_t)r.splits * units;
+            r.splits = __builtin_amdgcn_readlane(s, l);
+            r.live = __builtin_amdgcn_readlane(live, l);
+            r.first = __builtin_amdgcn_readlane(upto, l) - ((r.splits - 1) * r.live + a.tiles) * H;
+            const int even = (__builtin_amdgcn_readlane(blocks, l) + r.splits - 1) / r.splits;
+            r.per = min(r.per, (even + LEAST - 1) / LEAST * LEAST);
+            if (a.split && r.first == find && threadIdx.x == 0) a.plan[r.b] = make_int4(r.live, r.splits, r.first, 0);
             return r;
         }
-        base = __shfl(upto, 63);
+        base = __builtin_amdgcn_readlane(upto, 63);
     }
-    r.b = c.batch;
-    r.splits = 0;
-    r.first = 0;
+    r.b = batch;
+    r.live = r.splits = r.first = 0;
     return r;
 }
 
@@ -504,17 +554,22 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
         from = split * per;
         to = min(a.w + 1, from + per);
     } else {
-        const int units = a.tiles * H;
-        const KvRange r = kv_plan(a.c, units, a.target, blockIdx.x, 0);
+        const KvRange r = kv_plan<16>(a, blockIdx.x);
         if (r.b >= a.c.batch) return;
         b = r.b;
-        splits = r.splits;
-        const int local = (int)(blockIdx.x - r.first);
+        const int local = (int)blockIdx.x - r.first, units = r.live * H, pad = local - units * r.splits;
         slot = blockIdx.x;
-        h = local % H;
-        tile = local / H % a.tiles;
-        from = local / units * r.per;
-        to = from + r.per;
+        h = (pad < 0 ? local : pad) % H;
+        if (pad < 0) {
+            splits = r.splits;
+            tile = local / H % r.live;
+            from = local / units * r.per;
+            to = from + r.per;
+        } else {  // rows of padding: zeros
+            splits = 1;
+            tile = r.live + pad / H;
+            from = to = 0;
+        }
     }
     b = __builtin_amdgcn_readfirstlane(b);
     const int64_t bh = (int64_t)b * H + h;
@@ -815,13 +870,15 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     constexpr int LOADS = KB * D / 16 / 256 + (KB * D / 16 % 256 ? 1 : 0);  // pieces of a thread, of keys and of values
     __shared__ u32x4 s_k[2][KB * D / 16], s_v[2][KB * D / 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
-    const int H = a.c.heads, g = a.g, units = a.tiles * H;
-    const KvRange r = kv_plan(a.c, units, a.target, blockIdx.x, 0);
+    const int H = a.c.heads, g = a.g;
+    const KvRange r = kv_plan<128>(a, blockIdx.x);
     if (r.b >= a.c.batch) return;
-    const int b = __builtin_amdgcn_readfirstlane(r.b), splits = r.splits;
-    const int local = __builtin_amdgcn_readfirstlane((int)(blockIdx.x - r.first));
-    const int h = local % H, tile = a.tiles - 1 - local / H % a.tiles;  // the longest ones first
-    const int64_t bh = (int64_t)b * H + h, slot = r.first + local / units * units + tile * H + h;
+    const int b = __builtin_amdgcn_readfirstlane(r.b), units = r.live * H;
+    const int local = __builtin_amdgcn_readfirstlane((int)blockIdx.x - r.first), pad = local - units * r.splits;
+    const int h = (pad < 0 ? local : pad) % H, splits = pad < 0 ? r.splits : 1;
+    const int tile = pad < 0 ? r.live - 1 - local / H % r.live : r.live + pad / H;  // the longest ones first; rows of padding last
+    const int range = pad < 0 ? local / units : 0;
+    const int64_t bh = (int64_t)b * H + h, slot = r.first + range * units + tile * H + h;
     const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n), nb = len / KB;
     auto seen_by = [&](int row) {  // what the row sees; rows past the last one like it
         const int i = min(row, a.n * g - 1) / g;
@@ -838,8 +895,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
         return from < a.n * g && i0 < count ? max(0, len - count + i1 + 1) : 0;
     };
     const int most = most_of(row0, ROWS), wmost = most_of(wrow, 32), wleast = wrow < a.n * g ? seen_by(wrow) : 0;
-    int from = local / units * r.per;
-    const int to = min(from + r.per, MASS ? (len + KB - 1) / KB : (most + KB - 1) / KB);
+    const int from = range * r.per;
+    const int to = pad < 0 ? min(from + r.per, MASS ? (len + KB - 1) / KB : (most + KB - 1) / KB) : 0;
 
     typename T::x8 q[2 * PAIRS];
     const uint16_t *qp = a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + ((int64_t)h * g + hg) * a.qs[2];
@@ -1054,12 +1111,11 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a)
         slot = unit;
         step = a.units;
     } else {
-        const int units = a.tiles * H;
-        b = (int)(unit / units);
-        const KvRange r = kv_plan(a.c, units, a.target, -1, b);
-        splits = r.splits;
-        slot = r.first + tile * H + h;
-        step = units;
+        b = (int)(unit / (a.tiles * H));
+        const int4 r = a.plan[b];  // live tiles, ranges, first workgroup
+        splits = tile < r.x ? r.y : 1;
+        slot = r.z + tile * H + h;
+        step = r.x * H;
     }
     if (splits < 2) return;
     const int row = LIST ? token * g + tile * ROWS + y : tile * ROWS + y;
