@@ -112,7 +112,7 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         // enough workgroups for the card, none with less than a block to a wave
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((w + 1) / KV_LEAST, 512 / std::max<int64_t>(1, p.units)));
         p.solo = p.units >= 2048;
-        p.grid = p.solo ? (p.units + 3) / 4 : p.units * p.splits;
+        p.grid = p.solo ? (p.units / c->heads + 3) / 4 * c->heads : p.units * p.splits;
     } else {
         p.many = rows > 64;
         p.rows = p.many ? 128 : 16;
