@@ -121,7 +121,10 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         // up to KV_ROUNDS rounds of workgroups (kv_plan) and one for each unit of a sequence; a card full of workgroups from the tiles of prompts alone
         // needs no ranges
         const int64_t units = c->batch * p.units;
-        p.split = !p.many || units < 1024;
+        // Short tables are no faster in ranges, which cost the join's launch.  Single tokens, 8 heads, in a graph: one sequence of 500
+        // tokens 8.6 us without and 10.3 with ranges, 1000 tokens 11.3 and 10.4 (but 14 and 16.5 called one by one), 2000 tokens 16.8
+        // and 10.4; 16 sequences of 1000 tokens 13.2 and 18.3, 2000 tokens 19.4 and 22.6, 4000 tokens 30.1 and 31.7.
+        p.split = p.many ? units < 1024 : c->max_blocks > (units >= 128 ? 32 : 16);
         p.grid = (p.split ? KV_ROUNDS * KV_ROUND : 0) + units;
     }
     const bool parts = w > 0 ? p.splits > 1 : p.split;
