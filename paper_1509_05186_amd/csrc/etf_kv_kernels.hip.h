@@ -9,6 +9,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -87,6 +89,8 @@ __device__ __forceinline__ int64_t kv_tail(const KvView &c, int64_t bh, int b, i
 // The workgroup of the first block reads the open block's earlier tokens; it also writes what is left over into the open
 // block, afterwards, because both may be the same buffer.  A token that is not finite has keys that are not numbers
 // and values of zero: rows that see it become not a number, others do not.
+// Bound by vector issue and memory alike: four prompts of 8192 tokens, 8 heads of 128 dimensions (202 MB) 48 us = 4.2 TB/s; with maxima and
+// bounds number by number instead of two to an operation 53 us.
 // ------------------------------------------------------------------------------------------------
 struct KvAppendArgs {
     KvView c;
@@ -96,41 +100,30 @@ struct KvAppendArgs {
     int n, per;  // per: workgroups of a (sequence, head), the most blocks that n tokens can complete
 };
 
-// a code's place in the order of the values
-__device__ __forceinline__ int code_order(uint32_t u)
+// Largest size of eight numbers, as the bits without the sign, which are in the order of the sizes; from T::EXP on: one of them is not finite
+__device__ __forceinline__ uint32_t size8(const uint4 &w)
 {
-    const int m = (int)(u & 0x7F);
-    return u & 0x80 ? -m : m;
-}
-__device__ __forceinline__ uint8_t code_of_order(int m) { return (uint8_t)(m < 0 ? 0x80 | -m : m); }
-
-template <typename T>
-__device__ __forceinline__ bool all_finite(const uint4 &w)
-{
-    constexpr uint32_t lo = T::EXP, hi = T::EXP << 16;
-    bool ok = true;
-    for (uint32_t u : {w.x, w.y, w.z, w.w}) ok = ok && (u & lo) != lo && (u & hi) != hi;
-    return ok;
+    constexpr uint32_t mask = 0x7FFF7FFFu;
+    const u16x2 a = __builtin_bit_cast(u16x2, w.x & mask), b = __builtin_bit_cast(u16x2, w.y & mask);
+    const u16x2 c = __builtin_bit_cast(u16x2, w.z & mask), d = __builtin_bit_cast(u16x2, w.w & mask);
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(a, b), __builtin_elementwise_max(c, d));
+    return max((uint32_t)m[0], (uint32_t)m[1]);
 }
 
-template <typename T>
-__device__ __forceinline__ float amax8(const uint4 &w)
-{
-    float m = 0.f;
-    for (uint32_t u : {w.x, w.y, w.z, w.w}) m = fmaxf(m, fmaxf(fabsf(T::wide((uint16_t)u)), fabsf(T::wide((uint16_t)(u >> 16)))));
-    return m;
-}
+// Codes in the order of their values, two to a word: 16-bit numbers whose low byte is the code, its lower bits turned where it is
+// negative (so that -0 stands below +0).  Its own inverse.
+__device__ __forceinline__ i16x2 code_order(i16x2 code) { return code ^ ((code >> 15) & (int16_t)0x7F); }
 
-// eight values times 2^-e as codes
+// eight values times `inverse`, a power of two, as codes
 template <typename T>
-__device__ __forceinline__ uint2 codes8(const uint4 &w, int e)
+__device__ __forceinline__ uint2 codes8(const uint4 &w, float inverse)
 {
     uint32_t o[2];
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
     for (int i = 0; i < 2; ++i) {
         float f[4];
         // beyond 448 only where the scale is the largest: the code of the largest value then
-        for (int j = 0; j < 4; ++j) f[j] = fminf(fmaxf(ldexpf(T::wide((uint16_t)(in[2 * i + j / 2] >> (16 * (j & 1)))), -e), -448.f), 448.f);
+        for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_fmed3f(T::wide((uint16_t)(in[2 * i + j / 2] >> (16 * (j & 1)))) * inverse, -448.f, 448.f);
         const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
         o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], lo, true);
     }
@@ -155,7 +148,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     constexpr int VROW = KB + 4;             // LDS row of one dimension's value codes, padded
     __shared__ __attribute__((aligned(16))) uint8_t s_v[D * VROW];
     __shared__ __attribute__((aligned(16))) uint8_t s_k[KB * D];
-    __shared__ float s_amax[2][4];
+    __shared__ uint32_t s_amax[2][4];
     __shared__ int s_bad[KB];
     constexpr int BW = D / 4, BG = 256 / BW, BT = (KB + BG - 1) / BG;  // bounds: words of a row, groups of tokens, tokens of a group
     __shared__ __attribute__((aligned(8))) int16_t s_edge[2][BG][D];
@@ -172,6 +165,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     if (blk < full) {
         const int64_t old = kv_tail(a.c, bh, b, first, D);
         uint4 kw[NP], vw[NP];
+        uint32_t ks[NP], vs[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
@@ -185,34 +179,37 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
                 for (int j = 0; j < 8; ++j) x[j] = a.c.tail_v[old + (d + j) * KB + t];
                 vw[i] = make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
             }
-            if (!all_finite<T>(kw[i]) || !all_finite<T>(vw[i])) s_bad[t] = 1;
+            ks[i] = size8(kw[i]);
+            vs[i] = size8(vw[i]);
+            if (max(ks[i], vs[i]) >= T::EXP) s_bad[t] = 1;
         }
         __syncthreads();
-        float mk = 0.f, mv = 0.f;
+        uint32_t mk = 0, mv = 0;
         bool bad[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             bad[i] = s_bad[(tid + 256 * i) / PT] != 0;
             if (!bad[i]) {
-                mk = fmaxf(mk, amax8<T>(kw[i]));
-                mv = fmaxf(mv, amax8<T>(vw[i]));
+                mk = max(mk, ks[i]);
+                mv = max(mv, vs[i]);
             }
         }
         for (int o = 32; o; o >>= 1) {
-            mk = fmaxf(mk, __shfl_xor(mk, o));
-            mv = fmaxf(mv, __shfl_xor(mv, o));
+            mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
+            mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
         }
         if (lane == 0) {
             s_amax[0][wave] = mk;
             s_amax[1][wave] = mv;
         }
         __syncthreads();
-        const int ek = scale_exponent(fmaxf(fmaxf(s_amax[0][0], s_amax[0][1]), fmaxf(s_amax[0][2], s_amax[0][3])));
-        const int ev = scale_exponent(fmaxf(fmaxf(s_amax[1][0], s_amax[1][1]), fmaxf(s_amax[1][2], s_amax[1][3])));
+        const int ek = scale_exponent(T::wide((uint16_t)max(max(s_amax[0][0], s_amax[0][1]), max(s_amax[0][2], s_amax[0][3]))));
+        const int ev = scale_exponent(T::wide((uint16_t)max(max(s_amax[1][0], s_amax[1][1]), max(s_amax[1][2], s_amax[1][3]))));
+        const float ik = ldexpf(1.f, -ek), iv = ldexpf(1.f, -ev);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
-            uint2 ck = codes8<T>(kw[i], ek), cv = codes8<T>(vw[i], ev);
+            uint2 ck = codes8<T>(kw[i], ik), cv = codes8<T>(vw[i], iv);
             if (bad[i]) {
                 ck = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
                 cv = make_uint2(0, 0);
@@ -231,21 +228,22 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
             // smallest and largest codes: four dimensions and a group of tokens to a thread, then the groups
             if (tid < BW * BG) {
                 const int w = tid % BW, grp = tid / BW;
-                int lo[4] = {0x7F, 0x7F, 0x7F, 0x7F}, hi[4] = {-0x7F, -0x7F, -0x7F, -0x7F};
+                i16x2 lo[2], hi[2];  // of bytes 0 and 2, of bytes 1 and 3
+                lo[0] = lo[1] = 0x7F;
+                hi[0] = hi[1] = -0x80;
                 for (int t = grp * BT; t < min(KB, (grp + 1) * BT); ++t) {
                     if (s_bad[t]) continue;
-                    const uint32_t u = *reinterpret_cast<const uint32_t *>(s_k + t * D + 4 * w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int o = code_order(u >> (8 * i));
-                        lo[i] = min(lo[i], o);
-                        hi[i] = max(hi[i], o);
-                    }
+                    const i16x2 u = *reinterpret_cast<const i16x2 *>(s_k + t * D + 4 * w);
+                    const i16x2 even = code_order((i16x2)(u << 8) >> 8), odd = code_order(u >> 8);
+                    lo[0] = __builtin_elementwise_min(lo[0], even);
+                    lo[1] = __builtin_elementwise_min(lo[1], odd);
+                    hi[0] = __builtin_elementwise_max(hi[0], even);
+                    hi[1] = __builtin_elementwise_max(hi[1], odd);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    s_edge[0][grp][4 * w + i] = (int16_t)lo[i];
-                    s_edge[1][grp][4 * w + i] = (int16_t)hi[i];
+                    s_edge[0][grp][4 * w + i] = lo[i & 1][i >> 1];
+                    s_edge[1][grp][4 * w + i] = hi[i & 1][i >> 1];
                 }
             }
             if (tid < 2) a.c.scales[(int64_t)page * 2 + tid] = ldexpf(1.f, tid ? ev : ek);
@@ -256,13 +254,14 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
             uint32_t out = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                int lo = 0x7F, hi = -0x7F;
+                int lo = 0x7F, hi = -0x80;
                 for (int y = 0; y < BG; ++y) {
                     lo = min(lo, (int)s_edge[0][y][d + i]);
                     hi = max(hi, (int)s_edge[1][y][d + i]);
                 }
-                const int o = lo > hi ? 0 : e ? hi : lo;
-                out |= (uint32_t)code_of_order(o) << (8 * i);
+                const i16x2 o = {(int16_t)(lo > hi ? 0 : e ? hi : lo), 0};
+                const uint32_t code = (uint32_t)(uint16_t)code_order(o)[0] & 0xFF;
+                out |= (code == 0x80 ? 0 : code) << (8 * i);  // no -0
             }
             *reinterpret_cast<uint32_t *>(a.c.bounds + ((int64_t)page * 2 + e) * D + d) = out;
         }
@@ -281,7 +280,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
             const int at = full * KB + t - begin;
             uint4 kw = *reinterpret_cast<const uint4 *>(nk + at * a.ks[1] + d), vw = *reinterpret_cast<const uint4 *>(nv + at * a.vs[1] + d);
             if (pass == 0) {
-                if (!all_finite<T>(kw) || !all_finite<T>(vw)) s_bad[t] = 1;
+                if (max(size8(kw), size8(vw)) >= T::EXP) s_bad[t] = 1;
                 continue;
             }
             if (s_bad[t]) {
@@ -307,6 +306,8 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
 // 10.7 instead of 13.2 TB/s from the second-level cache); the next block's keys are asked for as soon as this one's are in
 // registers, the values likewise, so that a wave always has a block on its way.  A wave takes every fourth block of its workgroup's
 // range; the four join through LDS, ranges of a long cache through memory (k_kv_join).
+// Bound by memory: 820 MB of cache (four sequences of 100 000 tokens) at 5.5 TB/s, 545 MB (64 sequences of up to 8192) at 5.0; listed blocks of
+// many tokens by the second-level caches, 14.6 TB/s.
 // ------------------------------------------------------------------------------------------------
 struct KvAttendArgs {
     KvView c;
@@ -869,6 +870,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
 // row and p^T stands in its registers as the second product wants it: row m of a tile of s^T is token
 // 16 (m / 4 % 2) + 8 (m / 16) + 4 (m / 8 % 2) + m % 4 of its 32.  The next block is on its way from memory to registers while this one
 // is worked on.  Pieces of 16 bytes are exchanged within a row of LDS, so that eight lanes that read together hit all banks.
+// Bound by vector issue beside the matrix cores (64 % and 42 % of the time): two prompts of 4096 tokens, 32 heads of 128 dimensions 302 us =
+// 910 TFLOP/s.  Making operands of the codes once a workgroup, on their way into LDS, instead of in every wave: 306 us.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int D, bool MASS>
 __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
@@ -1203,7 +1206,8 @@ __global__ __launch_bounds__(256) void k_kv_mass(KvView c, const float *__restri
 // element and a code are exact in float32, D of them are not zero, and their float32 additions, rounded or truncated, are off by at most
 // D 2^-23 of the sum of the terms' sizes, a second product of the same shape.  k_kv_pick takes the choice from these scores and bounds, and evaluates
 // the blocks that they leave open in float64, where products of at most 15 bits add up to the same sum in any order
-// unless a query's elements differ by more than 2^20 in size.
+// unless a query's elements differ by more than 2^20 in size.  Chains of dependent loads and counts bound both: 13 and 14 us for 256 rows of up to 512
+// blocks, 16 and 34 for 8 rows of 15 625 (a row's keys on one compute unit), 30 and 29 for 8000 rows of 256.
 // ------------------------------------------------------------------------------------------------
 struct KvSelectArgs {
     KvView c;
@@ -1854,6 +1858,7 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
 // Eviction: of every (sequence, head) with more than `budget` blocks the first `sink`, the last `recent` and those of
 // the others with the largest weight stay, in their order.  Lengths that are changed in place change in a launch of their own
 // (k_kv_evict_lens), since every workgroup here reads them; into other arrays (lens_out not null) they are written here.
+// Bound by latency: 7 us for 128 rows of 128 blocks, 10 for 16 rows of 313.
 // ------------------------------------------------------------------------------------------------
 // Everything is read before anything is written, since the outputs may be the inputs; with more blocks than the registers hold a launch
 // of one workgroup per row has to write apart from what it reads (KPT = 0: `table_out` and `mass_out` are not the inputs).
