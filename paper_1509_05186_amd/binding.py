@@ -223,7 +223,8 @@ class KvCache:
     """An attention cache in 8 bits: the device tensors of an etf_kv_cache, which the caller owns.
 
     k, v, bounds: float8_e4m3fn [pages][64][D], [pages][D][64], [pages][2][D]; scales: float32 [pages][2]; tail_k, tail_v: bfloat16 or
-    float16 [B][H][2][64][D], [B][H][2][D][64]; table: int32 [B][H][max_blocks]; lens, evicted: int32 [B].
+    float16 [B][H][2][64][D], [B][H][2][D][64]; table: int32 [B][H][max_blocks]; lens, evicted: int32 [B].  Another tensor of the same
+    kind may be assigned to a field: the calls from then on use it.
     """
 
     FIELDS = ("k", "v", "scales", "bounds", "tail_k", "tail_v", "table", "lens", "evicted")
@@ -237,20 +238,23 @@ class KvCache:
         pages, T = k.shape[0], tail_k.dtype
         if T not in (torch.bfloat16, torch.float16):
             raise ValueError("open blocks are bfloat16 or float16, not %s" % T)
-        e4m3, S = torch.float8_e4m3fn, ETF_KV_BLOCK
-        want = dict(k=((pages, S, D), e4m3), v=((pages, D, S), e4m3), scales=((pages, 2), torch.float32), bounds=((pages, 2, D), e4m3),
-                    tail_k=((B, H, 2, S, D), T), tail_v=((B, H, 2, D, S), T), table=((B, H, table.shape[2]), torch.int32),
-                    lens=((B,), torch.int32), evicted=((B,), torch.int32))
-        for name, t in given.items():
-            shape, dtype = want[name]
-            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != k.device:
-                raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (name, dtype, list(shape), k.device))
-        self._t = given
         self.batch, self.heads, self.head_dim, self.max_blocks, self.pages, self.dtype, self.device = B, H, D, table.shape[2], pages, T, k.device
+        for name, t in given.items():
+            self._check(name, t)
+        self._t = given
         c = EtfKvCache(ETF_KV_BF16 if T == torch.bfloat16 else ETF_KV_FP16, B, H, D, table.shape[2], pages)
         for name in self.FIELDS:
             setattr(c, name, given[name].data_ptr())
         self._set(c)
+
+    def _check(self, name, t):
+        import torch
+        B, H, D, S, e4m3 = self.batch, self.heads, self.head_dim, ETF_KV_BLOCK, torch.float8_e4m3fn
+        shape, dtype = dict(k=((self.pages, S, D), e4m3), v=((self.pages, D, S), e4m3), scales=((self.pages, 2), torch.float32),
+                            bounds=((self.pages, 2, D), e4m3), tail_k=((B, H, 2, S, D), self.dtype), tail_v=((B, H, 2, D, S), self.dtype),
+                            table=((B, H, self.max_blocks), torch.int32), lens=((B,), torch.int32), evicted=((B,), torch.int32))[name]
+        if not isinstance(t, torch.Tensor) or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != self.device:
+            raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (name, dtype, list(shape), self.device))
 
     def _set(self, c):
         import torch
@@ -259,10 +263,19 @@ class KvCache:
         self._sizes = {}    # workspace bytes by call
         self._raw = self._t["lens"].new_empty(0, dtype=torch.uint8)    # of the kind that workspaces are
 
-    def __getattr__(self, name):
-        if name in KvCache.FIELDS:
-            return self.__dict__["_t"][name]
-        raise AttributeError(name)
+    def _field(name):
+        def get(self):
+            return self._t[name]
+
+        def put(self, t):
+            if t is not self._t[name]:    # `cache.lens += n` assigns the tensor that is there
+                self._check(name, t)
+                self._t[name] = t
+                setattr(self._c, name, t.data_ptr())
+        return property(get, put)
+
+    k, v, scales, bounds, tail_k, tail_v, table, lens, evicted = map(_field, FIELDS)
+    del _field
 
     @classmethod
     def alloc(cls, batch: int, heads: int, head_dim: int, max_tokens: int, dtype=None, pages: Optional[int] = None, device="cuda"):

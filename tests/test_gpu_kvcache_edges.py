@@ -1,0 +1,48 @@
+"""Attention over a cache in 8 bits on the GPU, where a call is easily wrong: a cache cut into a fork, against the oracle in float64; bounds as in
+test_gpu_kvcache.py unless a test states its own."""
+import os
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from oracle import kvcache as kv  # noqa: E402
+import paper_1509_05186_amd as etf  # noqa: E402
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+from test_gpu_kvcache import BF, HF, check_out, context, on_gpu, queries, same_cache, say  # noqa: E402
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_a_fork_of_a_cache_that_was_advanced_goes_on(dtype):
+    """Tokens come, the cache is cut into a fork, tokens come to the fork: what it holds and answers are the oracle's."""
+    say("fork", dtype)
+    D, H, B, blocks = 64, 2, 2, 8
+    g = torch.Generator().manual_seed(1)
+    c = kv.new_cache(B, H, D, blocks, dtype)
+    cache, ctx = on_gpu(c), context()
+
+    def come(cache, n):
+        k, v = (torch.randn(B, n, H, D, generator=g).to(dtype) for _ in range(2))
+        ctx.kv_append(cache, k.cuda(), v.cuda())
+        kv.append(c, k, v)
+        cache.lens += n
+        c["lens"] += n
+
+    come(cache, 410)
+    mass = torch.rand(B, H, blocks, generator=g)
+    to = cache.fork()
+    was = cache.lens.clone()
+    kept, freed = ctx.kv_evict(cache, mass.cuda(), 3, sink=1, recent=1, to=to)
+    table, lens, evicted, _, gone = kv.evict(c, mass, 3, 1, 1)
+    assert torch.equal(to.lens.cpu(), lens) and torch.equal(to.table.cpu(), table) and torch.equal(cache.lens, was)
+    table[:, :, 3:6] = gone[:, :, :3]      # pages that came free serve the next blocks
+    to.table.copy_(table)
+    c["table"], c["lens"], c["evicted"] = table, lens, evicted
+    come(to, 70)
+    assert torch.equal(cache.lens, was)
+    same_cache(to, c, "fork")
+    q = queries(g, dtype, B, 1, 2 * H, D)
+    check_out(kv.attend(c, q, D ** -0.5), ctx.kv_attend(to, q.cuda()), dtype, "fork")
