@@ -736,7 +736,8 @@ class Context:
         mine = self._stream or 0
         if _current_stream(cache._gpu) == mine:
             return torch.empty(shape, dtype=dtype, device=cache.device)
-        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=cache.device)):
+        # torch takes a stream of its pool for a pointer of zero
+        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=cache.device) if mine else torch.cuda.default_stream(cache.device)):
             return torch.empty(shape, dtype=dtype, device=cache.device)
 
     def _kv_scratch(self, cache: KvCache, call, *args):

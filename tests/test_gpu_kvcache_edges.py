@@ -46,3 +46,32 @@ def test_a_fork_of_a_cache_that_was_advanced_goes_on(dtype):
     same_cache(to, c, "fork")
     q = queries(g, dtype, B, 1, 2 * H, D)
     check_out(kv.attend(c, q, D ** -0.5), ctx.kv_attend(to, q.cuda()), dtype, "fork")
+
+
+def test_a_context_on_the_default_stream_called_under_another(monkeypatch):
+    say("default stream")
+    D, H, B = 64, 2, 2
+    g = torch.Generator().manual_seed(2)
+    c = kv.new_cache(B, H, D, 12, BF)
+    k, v = (torch.randn(B, 700, H, D, generator=g).to(BF) for _ in range(2))
+    kv.append(c, k, v)
+    c["lens"] += 700
+    q = queries(g, BF, B, 1, 4 * H, D)
+    want, blocks = kv.attend(c, q, D ** -0.5), kv.select(c, q, 4, 1, 1)
+    listed = kv.attend(c, q, D ** -0.5, lists=blocks)
+    cache, gq, side = on_gpu(c), q.cuda(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    made, empty = [], torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: made.append(torch.cuda.current_stream().cuda_stream) or empty(*a, **k))
+    for ctx in (etf.Context(device=0), etf.Context(device=0, stream=torch.cuda.default_stream().cuda_stream)):
+        for _ in range(3):
+            with torch.cuda.stream(side):
+                out = ctx.kv_attend(cache, gq)
+                lists = ctx.kv_select(cache, gq, 4, sink=1, recent=1)
+                some = ctx.kv_attend(cache, gq, lists=lists)
+                torch.randn(1 << 20, device="cuda").mul_(2)          # work of the program's stream
+            torch.cuda.synchronize()
+            check_out(want, out, BF, "default stream")
+            assert torch.equal(lists.cpu(), blocks)
+            check_out(listed, some, BF, "default stream, listed")
+    assert len(made) == 2 * 3 * 6 and set(made) == {torch.cuda.default_stream().cuda_stream}
