@@ -771,6 +771,8 @@ class Context:
         pq, sq = self._rows(q, cache, None, "q")
         B, n, heads_q, D = q.shape
         w = 0 if lists is None else lists.shape[-1]
+        if lists is not None and w == 0:
+            raise ValueError("lists: expected an entry at least (None: all tokens)")
         pl = self._kv_dev(lists, (B, n, cache.heads, w), torch.int32, cache, "lists")
         pc = self._kv_dev(counts, (B,), torch.int32, cache, "counts")
         if out is None:

@@ -1,0 +1,27 @@
+"""Arguments that the cache calls refuse or take, before anything reaches a GPU (no GPU: what is taken ends with its absence, code -5)."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from oracle import kvcache as kv  # noqa: E402
+import paper_1509_05186_amd as etf  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def made():
+    ctx, c = etf.Context(device=None), etf.KvCache(**kv.new_cache(2, 3, 64, 4, torch.bfloat16))
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    q = torch.zeros(2, 1, 6, 64, dtype=torch.bfloat16)
+    return ctx, c, q, dict(out=torch.empty_like(q), ws=ws)
+
+
+def taken(call, *args, **kw):
+    with pytest.raises(etf.EtfError) as e:
+        call(*args, **kw)
+    assert e.value.code == -5
+
+
+def test_lists_without_an_entry_are_not_all_tokens(made):
+    ctx, c, q, room = made
+    taken(ctx.kv_attend, c, q, lists=torch.zeros(2, 1, 3, 1, dtype=torch.int32), **room)
+    with pytest.raises(ValueError, match="lists"):
+        ctx.kv_attend(c, q, lists=torch.zeros(2, 1, 3, 0, dtype=torch.int32), **room)
