@@ -723,6 +723,13 @@ class Context:
         return t.data_ptr(), (ctypes.c_int64 * 3)(s[0], s[1], s[2])
 
     @staticmethod
+    def _no_gradient(t, what: str):
+        if t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise ValueError("%s requires a gradient, and the cache calls have none: detach it, or call them under torch.no_grad()" % what)
+
+    @staticmethod
     def _kv_dev(t, shape, dtype, cache: KvCache, what: str):
         if t is None:
             return None
@@ -751,9 +758,11 @@ class Context:
         return self._kv_empty((size,), torch.uint8, cache)
 
     def kv_append(self, cache: KvCache, k, v, counts=None):
-        """Writes new tokens k, v [B][n][H][D] after cache.lens; the caller then advances cache.lens."""
+        """Writes new tokens k, v [B][n][H][D] after cache.lens; the caller then advances cache.lens.  There is no gradient."""
         import torch
         self._kv_here(cache)
+        self._no_gradient(k, "k")
+        self._no_gradient(v, "v")
         pk, sk = self._rows(k, cache, cache.heads, "k")
         pv, sv = self._rows(v, cache, cache.heads, "v")
         if v.shape[1] != k.shape[1]:
@@ -765,9 +774,11 @@ class Context:
         return self._ck(self._lib.etf_kv_attend_workspace_bytes(self._h, cache._ref, n, heads_q, w, int(mass)))
 
     def kv_attend(self, cache: KvCache, q, scale: Optional[float] = None, counts=None, lists=None, out=None, lse=None, mass_in=None, mass_out=None, ws=None):
-        """Attention of q [B][n][heads_q][D] over the cache, over the blocks of lists (kv_select) if given.  scale: 1 / sqrt(D) by default."""
+        """Attention of q [B][n][heads_q][D] over the cache, over the blocks of lists (kv_select) if given.  scale: 1 / sqrt(D) by default.
+        There is no gradient: tensors that require one are refused where torch would record it."""
         import torch
         self._kv_here(cache)
+        self._no_gradient(q, "q")
         pq, sq = self._rows(q, cache, None, "q")
         B, n, heads_q, D = q.shape
         w = 0 if lists is None else lists.shape[-1]

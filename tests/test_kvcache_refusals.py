@@ -25,3 +25,21 @@ def test_lists_without_an_entry_are_not_all_tokens(made):
     taken(ctx.kv_attend, c, q, lists=torch.zeros(2, 1, 3, 1, dtype=torch.int32), **room)
     with pytest.raises(ValueError, match="lists"):
         ctx.kv_attend(c, q, lists=torch.zeros(2, 1, 3, 0, dtype=torch.int32), **room)
+
+
+def test_no_gradient_is_lost_in_silence(made):
+    ctx, c, q, room = made
+    grad = q.clone().requires_grad_()
+    new = torch.zeros(2, 1, 3, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="gradient"):
+        ctx.kv_attend(c, grad, **room)
+    for k, v in ((new.clone().requires_grad_(), new), (new, new.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="gradient"):
+            ctx.kv_append(c, k, v)
+        with torch.no_grad():
+            taken(ctx.kv_append, c, k, v)
+        taken(ctx.kv_append, c, k.detach(), v.detach())
+    with torch.no_grad():
+        taken(ctx.kv_attend, c, grad, **room)
+    taken(ctx.kv_attend, c, grad.detach(), **room)
+    taken(ctx.kv_select, c, grad, 2, ws=room["ws"], lists=torch.empty(2, 1, 3, 2, dtype=torch.int32))     # block numbers have no gradient
