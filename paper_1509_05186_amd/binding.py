@@ -720,7 +720,8 @@ class Context:
         s = t.stride()
         if s[3] != 1:
             raise ValueError("%s: a row's elements must be contiguous" % what)
-        return t.data_ptr(), (ctypes.c_int64 * 3)(s[0], s[1], s[2])
+        # of a dimension of one torch allows any stride, which nothing uses
+        return t.data_ptr(), (ctypes.c_int64 * 3)(*(s[i] if t.shape[i] > 1 else 0 for i in range(3)))
 
     @staticmethod
     def _no_gradient(t, what: str):

@@ -43,3 +43,18 @@ def test_no_gradient_is_lost_in_silence(made):
         taken(ctx.kv_attend, c, grad, **room)
     taken(ctx.kv_attend, c, grad.detach(), **room)
     taken(ctx.kv_select, c, grad, 2, ws=room["ws"], lists=torch.empty(2, 1, 3, 2, dtype=torch.int32))     # block numbers have no gradient
+
+
+def test_strides_that_no_row_uses_are_not_asked_about(made):
+    ctx, c, q, room = made
+    wide = torch.zeros(2, 4, 6, 68, dtype=torch.bfloat16)          # rows of 68 elements: no stride of 8
+    with pytest.raises(etf.EtfError) as e:
+        ctx.kv_attend(c, wide[:, :1, :, :64], **room)
+    assert e.value.code == -1
+    one = etf.KvCache(**kv.new_cache(1, 1, 64, 4, torch.bfloat16))
+    lone = torch.zeros(4 * 132, dtype=torch.bfloat16).as_strided((1, 1, 2, 64), (131, 68, 72, 1))     # one sequence, one token
+    assert not lone.is_contiguous()
+    out = torch.empty(1, 1, 2, 64, dtype=torch.bfloat16)
+    taken(ctx.kv_attend, one, lone, out=out, ws=room["ws"])
+    taken(ctx.kv_append, one, lone[:, :, :1].expand(1, 3, 1, 64), torch.zeros(600, dtype=torch.bfloat16).as_strided((1, 3, 1, 64), (1, 136, 3, 1)))
+    taken(ctx.kv_select, one, lone, 2, ws=room["ws"], lists=torch.empty(1, 1, 1, 2, dtype=torch.int32))
