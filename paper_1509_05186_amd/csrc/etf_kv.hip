@@ -17,7 +17,8 @@ namespace {
 inline int64_t al256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
-constexpr int64_t GRID_MOST = 0x7FFFFFFF;
+// a launch has fewer than 2^32 threads
+inline bool too_many(int64_t groups, int threads = 256) { return groups > (int64_t)UINT32_MAX / threads; }
 constexpr int KV_EVICT_MOST = 16384;  // blocks of a row that a workgroup of k_kv_evict holds
 
 // arrays: the call goes to the device and reads them
@@ -190,7 +191,7 @@ extern "C" int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void
     const int64_t most = std::max(1, (KB - 1 + n) / KB);  // blocks that n tokens can complete
     a.per = (int)most;
     const int64_t grid = (int64_t)cache->batch * cache->heads * most;
-    if (grid > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many blocks for one call");
+    if (too_many(grid)) return fail(ctx, ETF_EINVAL, "too many blocks for one call");
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     return with_shape(cache, [&](auto t, auto dim) {
         ProfScope prof(ctx, ETF_K_KV);
@@ -228,7 +229,12 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
     KvAttendArgs a{};
     a.c = view_of(cache);
     if ((rc = check_rows(ctx, cache, "q", q, q_strides, n, heads_q, a.qs)) != ETF_OK) return rc;
-    if (p.grid > GRID_MOST || (lists ? 2 * p.units : cache->batch * p.units * (p.rows / 8)) > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    // lanes of a block's weight (k_kv_mass)
+    int width = 1;
+    while (width < 256 && width < n * (heads_q / cache->heads)) width *= 2;
+    const int64_t blocks = (int64_t)cache->batch * cache->heads * cache->max_blocks, mass_grid = (blocks + 256 / width - 1) / (256 / width);
+    const int64_t joins = lists ? p.splits > 1 ? 2 * p.units : 0 : p.split ? cache->batch * p.units * (p.rows / 8) : 0;
+    if (too_many(p.grid) || too_many(joins) || (mass_out && too_many(mass_grid))) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     char *base = (char *)ws;
     a.q = (const uint16_t *)q;
     a.counts = counts;
@@ -256,11 +262,8 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
         return mass_out ? launch_attend<T, D, false, true>(ctx, a, p) : launch_attend<T, D, false, false>(ctx, a, p);
     });
     if (rc != ETF_OK || !mass_out) return rc;
-    int width = 1;
-    while (width < 256 && width < n * a.g) width *= 2;
-    const int64_t blocks = (int64_t)cache->batch * cache->heads * cache->max_blocks, grid = (blocks + 256 / width - 1) / (256 / width);
     ProfScope prof(ctx, ETF_K_KV);
-    hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, width, mass_in, mass_out);
+    hipLaunchKernelGGL(k_kv_mass, dim3((unsigned)mass_grid), dim3(256), 0, (hipStream_t)ctx->stream, a.c, a.row_lse, a.block_lse, n * a.g, width, mass_in, mass_out);
     LAUNCH_CHECK(ctx, "k_kv_mass");
     return ETF_OK;
 }
@@ -306,7 +309,8 @@ extern "C" int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void
     // a wave keeps its blocks' bounds for several tiles of tokens, as long as there are workgroups for every compute unit
     a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(8, chunks * a.tiles / 1024));
     const int64_t grid = chunks * ((a.tiles + a.turns - 1) / a.turns);
-    if (grid > GRID_MOST || rows > GRID_MOST) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    const bool many = cache->max_blocks <= 1024 ? too_many((rows + 3) / 4) : too_many(rows, cache->max_blocks <= 4096 ? 256 : 1024);
+    if (too_many(grid) || many) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     ProfScope prof(ctx, ETF_K_KV);
     return with_shape(cache, [&](auto t, auto dim) {
@@ -342,10 +346,12 @@ extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float
     if (!mass || !table_out || !lens_out || !evicted_out || !mass_out || !freed) return fail(ctx, ETF_EINVAL, "null pointer");
     if (cache->max_blocks > KV_EVICT_MOST && (table_out == cache->table || mass_out == mass))
         return fail(ctx, ETF_EINVAL, "tables of more than %d blocks are not cut in place", KV_EVICT_MOST);
+    const int64_t rows = (int64_t)cache->batch * cache->heads;
+    if (too_many(rows, cache->max_blocks <= 256 ? 64 : cache->max_blocks <= 4096 ? 256 : 1024)) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     ProfScope prof(ctx, ETF_K_KV);
     const KvView c = view_of(cache);
-    const dim3 grid((unsigned)(cache->batch * cache->heads));
+    const dim3 grid((unsigned)rows);
     hipStream_t st = (hipStream_t)ctx->stream;
     const bool apart = lens_out != cache->lens && evicted_out != cache->evicted && lens_out != cache->evicted && evicted_out != cache->lens;
     int32_t *lens = apart ? lens_out : nullptr;
