@@ -542,8 +542,8 @@ typedef struct etf_kv_cache {
 } etf_kv_cache;
 
 /* Writes the new tokens at [lens, lens + counts) of every sequence: into the open block, and as codes into the pages of the
- * blocks that they complete, for which table must have entries; lens stays as it is.  Tokens past the table's end are
- * dropped.  A token with a key or value that is not finite is kept with keys that are not numbers and values of zero:
+ * blocks that they complete, for which table must have entries; lens stays as it is.  Tokens from 64 max_blocks + 63 on, which lens does
+ * not count, are dropped.  A token with a key or value that is not finite is kept with keys that are not numbers and values of zero:
  * rows that see it become not a number, no others do, and its block's scales and bounds leave it out. */
 int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v,
                   const int64_t *v_strides, int n, const int32_t *counts);

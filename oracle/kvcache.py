@@ -47,10 +47,11 @@ def _page(c, b, h, j):
 
 
 def append(c, k, v, counts=None):
-    """Writes k, v [B][n][H][D] after c["lens"]; lens stays."""
+    """Writes k, v [B][n][H][D] after c["lens"], as far as lens can count; lens stays."""
     B, n, H, D = k.shape
     for b in range(B):
         count = n if counts is None else min(max(int(counts[b]), 0), n)
+        count = min(count, c["table"].shape[2] * BLOCK + BLOCK - 1 - _len(c, b))
         first, begin = _len(c, b) // BLOCK, _len(c, b) % BLOCK
         for h in range(H):
             old = (first + int(c["evicted"][b])) % 2
@@ -73,8 +74,6 @@ def append(c, k, v, counts=None):
                     if name == "k":
                         for w, edge in enumerate((code[ok].amin(0), code[ok].amax(0)) if ok.any() else (torch.zeros(D),) * 2):
                             c["bounds"][page, w] = edge.to(torch.float32).to(torch.float8_e4m3fn)
-            if first + whole > c["table"].shape[2]:
-                continue
             now, left = (first + whole + int(c["evicted"][b])) % 2, len(kk) - whole * BLOCK
             at = 0 if whole else begin
             c["tail_k"][b, h, now, at:left] = kk[whole * BLOCK + at:]

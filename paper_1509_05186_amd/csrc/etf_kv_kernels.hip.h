@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t bh = blockIdx.x / a.per;
     const int h = (int)(bh % a.c.heads), b = (int)(bh / a.c.heads), blk = blockIdx.x % a.per;
-    const int len = kv_len(a.c, b), count = kv_count(a.counts, b, a.n);
+    const int len = kv_len(a.c, b), count = min(kv_count(a.counts, b, a.n), a.c.blocks * KB + KB - 1 - len);  // as many as lens can count
     const int first = len / KB, begin = len % KB;
     const int full = (begin + count) / KB, left = (begin + count) % KB;
     if (blk > 0 && blk >= full) return;
@@ -270,7 +270,6 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     // what is left over: tokens [from, left) of the open block
     const int from = full ? 0 : begin;
     const int64_t now = kv_tail(a.c, bh, b, first + full, D);
-    if (first + full > a.c.blocks) return;  // no room: len stops before this
     if (tid < KB) s_bad[tid] = 0;
     __syncthreads();
     const int np = (left - from) * PT;

@@ -75,3 +75,24 @@ def test_a_context_on_the_default_stream_called_under_another(monkeypatch):
             assert torch.equal(lists.cpu(), blocks)
             check_out(listed, some, BF, "default stream, listed")
     assert len(made) == 2 * 3 * 6 and set(made) == {torch.cuda.default_stream().cuda_stream}
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 96)])
+@pytest.mark.parametrize("lens,n", [([64 * 3 + 10, 0], 60), ([64 * 3 - 10, 64 * 3 + 62], 100), ([0, 64 * 2], 400)])
+def test_append_past_the_tables_end(dtype, D, lens, n):
+    """Tokens that the lengths count are written, also by a call that goes on past them."""
+    say("past the end", dtype, D, lens, n)
+    B, H, blocks = 2, 2, 3
+    g = torch.Generator().manual_seed(n)
+    c = kv.new_cache(B, H, D, blocks, dtype)
+    kv.append(c, *(torch.randn(B, max(lens), H, D, generator=g).to(dtype) for _ in range(2)), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    cache = on_gpu(c)
+    k, v = (torch.randn(B, n, H, D, generator=g).to(dtype) for _ in range(2))
+    context().kv_append(cache, k.cuda(), v.cuda())
+    kv.append(c, k, v)
+    same_cache(cache, c, "past the end")
+    cache.lens += n
+    c["lens"] += n
+    q = queries(g, dtype, B, 1, 2 * H, D)
+    check_out(kv.attend(c, q, D ** -0.5), context().kv_attend(cache, q.cuda()), dtype, "past the end")
