@@ -96,3 +96,50 @@ def test_append_past_the_tables_end(dtype, D, lens, n):
     c["lens"] += n
     q = queries(g, dtype, B, 1, 2 * H, D)
     check_out(kv.attend(c, q, D ** -0.5), context().kv_attend(cache, q.cuda()), dtype, "past the end")
+
+
+def tight(r, D, dtype, below):
+    """Bounds as in test_gpu_kvcache.py, but weights smaller than 2^-14 of the largest held to the rounding of the others: those that the
+    kernels' factor leaves subnormal are off by `below` of the largest.  The output's own subnormal step stays."""
+    u = torch.finfo(dtype).eps / 2
+    delta = (D + 4) * 2.0 ** -24 * r["mag"]
+    w = (2 * delta + 4 * 2.0 ** -24 * (1 + r["reach"]) + r["seen"] * 2.0 ** -24)[..., None]
+    tol = (u + 2 * w) * r["size"] + u * r["out"].abs() + 1e-30
+    return tol + (below * (r["seen"] * r["vmax"])[..., None] + 2.0 ** -25 if dtype == HF else 0)
+
+
+def check_tight(r, out, dtype, below, what):
+    off, tol = (out.double().cpu() - r["out"]).abs(), tight(r, out.shape[-1], dtype, below)
+    assert (off <= tol).all(), "%s: %.3g over its bound" % (what, float((off / tol).max()))
+
+
+# bits by which the first token's weight is above the others': they are normal numbers next to it (2^-28 in tiles of 16 rows, 2^-20 in tiles of 128), or
+# subnormal ones, off by 2^-39 and 2^-31 of the largest at most
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,g,lens,bits", [(1, 4, [3000, 500], 20), (1, 4, [3000, 500], 27), (5, 3, [40, 900], 25), (90, 1, [2000, 91], 19), (20, 8, [1500, 20], 24), (90, 1, [20, 1000], 30)])
+def test_many_small_weights_next_to_a_large_one(dtype, n, g, lens, bits):
+    """The first token takes nearly all of the weight and has values of zero: what comes out is what the small weights add up to."""
+    say("small weights", dtype, n, g, lens, bits)
+    D, H, B = 64, 2, 2
+    rand = torch.Generator().manual_seed(bits)
+    c = kv.new_cache(B, H, D, max(lens) // 64 + 1, dtype)
+    k, v = torch.zeros(B, max(lens), H, D), torch.rand(B, max(lens), H, D, generator=rand) + 0.5
+    k[:, 1:, :, 1:3] = torch.randint(-4, 5, (B, max(lens) - 1, H, 2), generator=rand) / 8
+    k[:, 0, :, 0], v[:, 0] = 2.0, 0.0
+    kv.append(c, k.to(dtype), v.to(dtype), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    q = torch.zeros(B, n, g * H, D)
+    q[..., 0], q[..., 1:3] = bits * 4 * 0.6931, torch.randn(B, n, g * H, 2, generator=rand)
+    q, cache, ctx = q.to(dtype), on_gpu(c), context()
+    want = kv.attend(c, q, 0.125)
+    lse = torch.empty(q.shape[:3], device="cuda")
+    mass = torch.empty(c["table"].shape, device="cuda")
+    out = ctx.kv_attend(cache, q.cuda(), scale=0.125, lse=lse)
+    check_out(want, out, dtype, "small weights", lse)
+    out2 = ctx.kv_attend(cache, q.cuda(), scale=0.125, lse=lse, mass_out=mass)
+    check_out(want, out2, dtype, "small weights, weights of blocks", lse, mass)
+    below = 2.0 ** (-31 if n * g > 64 else -39)
+    check_tight(want, out, dtype, below, "small weights")
+    check_tight(want, out2, dtype, below, "small weights, weights of blocks")
+    lists = torch.arange(c["table"].shape[2], dtype=torch.int32).expand(B, n, H, -1).contiguous()
+    check_tight(want, ctx.kv_attend(cache, q.cuda(), scale=0.125, lists=lists.cuda()), dtype, 2.0 ** -39, "small weights, listed")
