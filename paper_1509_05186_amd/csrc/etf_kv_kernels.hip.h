@@ -31,7 +31,7 @@ struct TBf {
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float wide(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
     static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
-    static constexpr float VHALF = 1.f;
+    static constexpr bool NARROW = false;
     static constexpr int UP = 0, TILE_UP = 0, TILE_LAG = 8;
 };
 struct THf {
@@ -47,8 +47,10 @@ struct THf {
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float wide(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
     static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
-    // a value near the type's largest may round up past it in 8 bits: values are taken at half their size
-    static constexpr float VHALF = 0.5f;
+    // A value near the type's largest may round up past it in 8 bits, 65504 to 256 codes of 256 = 65536: where values have that scale, half
+    // of it goes to the weights.  A code times any smaller scale is a number of the type: a multiple of its smallest, like the
+    // values that it was rounded from.
+    static constexpr bool NARROW = true;
     // Softmax weights are taken 2^UP times as large (2^TILE_UP and up to 2^TILE_LAG more in k_kv_tile), the sums of them too: next to a
     // weight of 1 those below 2^-14 would lose bits and those below 2^-25 be gone, of which a long cache can have many.  So a weight is off
     // by 2^-39 of the largest at most (2^-31), besides its rounding.  2^10 and 2^4 in k_kv_tile: 135.7 instead of 134.7 us for pieces of
@@ -737,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
     for (int u = 0; u < many; ++u) {
         const int j = __builtin_amdgcn_readlane(js, u & 63);
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[0]), u & 63)) * a.scale2;
-        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[1]), u & 63)) * T::VHALF;
+        float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[1]), u & 63));
         if ((u & 63) == 63) look(u + 1);
         const int pn = u + 1 < many ? __builtin_amdgcn_readlane(ps, (u + 1) & 63) : -1;
         if (page >= 0) {
@@ -760,7 +762,12 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
                 }
             }
             softmax(s, ks, j, (j + 1) * KB <= least);
-            const typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+            typename T::x8 p0 = pack(s, 0), p1 = pack(s, 1);
+            if (T::NARROW && vs > 128.f) {
+                vs *= 0.5f;
+                p0 = p0 + p0;
+                p1 = p1 + p1;
+            }
             // this block's values, then the next one's keys
             if (pn >= 0)
                 wait_loads(LOADS);
@@ -810,7 +817,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
             for (int e = 0; e < 2; ++e) {
                 typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (i * 16 + x) * KB + 16 * hq + 8 * e);
 #pragma unroll
-                for (int y = 0; y < 8; ++y) v[y] = 8 * e + y < held ? v[y] * (decltype(v[0] + v[0]))T::VHALF : 0;
+                for (int y = 0; y < 8; ++y) v[y] = 8 * e + y < held ? v[y] : 0;
                 o[i] = T::mfma(v, e ? p1 : p0, o[i]);
             }
         }
@@ -827,7 +834,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
     if constexpr (SOLO) {
         if (!valid) return;
         const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg;
-        const float f = l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+        const float f = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
             const typename T::x2 p0 = T::narrow(o[i][0] * f, o[i][1] * f), p1 = T::narrow(o[i][2] * f, o[i][3] * f);
@@ -866,7 +873,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
                 a.part_ml[(slot * 16 + y) * 2 + 1] = all;
             }
         } else {
-            const float f = all != 0.f ? 1.f / (all * T::VHALF) : 0.f;
+            const float f = all != 0.f ? 1.f / all : 0.f;
             const int64_t at = ((int64_t)b * a.n + yi) * H * g + h * g + yh;
             const typename T::x2 p0 = T::narrow(sum[0] * f, sum[1] * f), p1 = T::narrow(sum[2] * f, sum[3] * f);
             *reinterpret_cast<uint2 *>(a.out + at * D + d) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
@@ -1025,7 +1032,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     for (int j = from; j < paged; ++j) {
         const int next = __builtin_amdgcn_readfirstlane(after);
         after = j + 2 < paged ? kv_page(a.c, bh, j + 2) : -1;
-        const float ks = next_scales[0], vs = next_scales[1] * T::VHALF;
+        const float ks = next_scales[0];
+        float vs = next_scales[1];
         if (next >= 0) fetch(next);
         if (page >= 0 && (MASS || j * KB < wmost)) {
             f32x16 s[2];
@@ -1043,6 +1051,12 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
             typename T::x8 p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = pack(s[i / 2], i % 2);
+            if (T::NARROW && __builtin_amdgcn_readfirstlane(__float_as_uint(vs)) > 0x43000000u) {  // above 128
+                asm volatile("");  // a branch: few blocks need it
+                vs *= 0.5f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = p[i] + p[i];
+            }
             if (next >= 0) stage(buf ^ 1);  // ahead of the second product rather than after it: 302 us instead of 309
 #pragma unroll
             for (int i = 0; i < DT; ++i)
@@ -1081,7 +1095,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
             for (int i = 0; i < DT; ++i) {
                 typename T::x8 v = *reinterpret_cast<const typename T::x8 *>(tv + (32 * i + x) * KB + at);
 #pragma unroll
-                for (int z = 0; z < 8; ++z) v[z] = z < held ? v[z] * (decltype(v[0] + v[0]))T::VHALF : 0;
+                for (int z = 0; z < 8; ++z) v[z] = z < held ? v[z] : 0;
                 o[i] = T::mfma(v, p, o[i]);
             }
         }
@@ -1096,7 +1110,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
         for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.f);
     }
     const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg, part = slot * ROWS + row - row0;
-    const float f = splits > 1 ? 1.f : l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+    const float f = splits > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -1175,7 +1189,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a)
             for (int i = 0; i < 8; ++i) o += v[i] * __shfl(weight, (threadIdx.x & 32) + i0 + i);
         }
     }
-    const float f = l != 0.f ? 1.f / (l * T::VHALF) : 0.f;
+    const float f = l != 0.f ? 1.f / l : 0.f;
     const int64_t at = ((int64_t)b * a.n + qi) * H * g + h * g + hg;
     const typename T::x2 p0 = T::narrow(o[0] * f, o[1] * f), p1 = T::narrow(o[2] * f, o[3] * f);
     if (lane < D / 4) *reinterpret_cast<uint2 *>(a.out + at * D + 4 * lane) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));

@@ -143,3 +143,28 @@ def test_many_small_weights_next_to_a_large_one(dtype, n, g, lens, bits):
     check_tight(want, out2, dtype, below, "small weights, weights of blocks")
     lists = torch.arange(c["table"].shape[2], dtype=torch.int32).expand(B, n, H, -1).contiguous()
     check_tight(want, ctx.kv_attend(cache, q.cuda(), scale=0.125, lists=lists.cuda()), dtype, 2.0 ** -39, "small weights, listed")
+
+
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("n,lens", [(1, [300, 64]), (1, [1500, 63]), (90, [400, 128])])
+@pytest.mark.parametrize("size", ["smallest", "small", "largest", "both"])
+def test_values_of_fp16_at_both_ends(D, n, lens, size):
+    """Values that are odd multiples of fp16's smallest number, and ones that round up past its largest in 8 bits (65504 to 65536), in full blocks and open ones:
+    no bit of them is lost on the way to the sum.  Bounds: those of small weights next to a large one; nothing for the values."""
+    say("ends", D, n, lens, size)
+    H, g, B = 2, 3, 2
+    rand = torch.Generator().manual_seed(D + n)
+    shape = (B, max(lens), H, D)
+    odd = (2 * torch.randint(-8, 8, shape, generator=rand) + 1) * 2.0 ** -24
+    big = torch.where(torch.rand(shape, generator=rand) < 0.5, -65504.0, 65504.0) * (torch.rand(shape, generator=rand) < 0.7)
+    v = dict(smallest=torch.full(shape, 2.0 ** -24), small=odd, largest=big, both=torch.where((torch.arange(max(lens)) // 64 % 2 == 0)[None, :, None, None], odd, big))[size]
+    k = torch.randn(shape, generator=rand)
+    c = kv.new_cache(B, H, D, max(lens) // 64 + 1, HF)
+    kv.append(c, k.half(), v.half(), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    q = queries(rand, HF, B, n, H * g, D, 0.0 if size == "smallest" else 1.0)
+    want = kv.attend(c, q, D ** -0.5)
+    cache, ctx, below = on_gpu(c), context(), 2.0 ** (-31 if n * g > 64 else -39)
+    check_tight(want, ctx.kv_attend(cache, q.cuda()), HF, below, "ends")
+    lists = torch.arange(c["table"].shape[2], dtype=torch.int32).expand(B, n, H, -1).contiguous()
+    check_tight(want, ctx.kv_attend(cache, q.cuda(), lists=lists.cuda()), HF, 2.0 ** -39, "ends, listed")
