@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <limits>
 
 #include "etf_internal.h"
 #include "etf_launch.h"
@@ -246,7 +247,7 @@ extern "C" int etf_kv_attend(etf_ctx *ctx, const etf_kv_cache *cache, const void
     a.plan = (int4 *)(base + p.o_plan);
     a.row_lse = (float *)(base + p.o_row);
     a.block_lse = (float *)(base + p.o_block);
-    a.scale2 = scale * 1.4426950408889634f;
+    a.scale2 = std::min(scale * 1.4426950408889634f, std::numeric_limits<float>::max());
     a.n = n;
     a.g = heads_q / cache->heads;
     a.w = w;

@@ -336,7 +336,7 @@ struct KvAttendArgs {
     float *part_o, *part_ml;  // partial results of ranges: [slot][rows of a tile][D], [slot][rows of a tile][2]
     int4 *plan;               // [b]: what k_kv_join needs of the sequence's ranges
     float *row_lse, *block_lse;  // logarithms (base 2) for the blocks' weights: [b][h][row], [b][h][blocks + 1][row]
-    float scale2;  // softmax scale times log2 e
+    float scale2;  // softmax scale times log2 e, finite
     int n, g, w, splits;
     int tiles;        // row tiles of a (sequence, head): of all tokens, or of one token where blocks are listed
     int64_t units;    // listed: (sequence, token, tile, head) units
@@ -437,6 +437,10 @@ __device__ __forceinline__ KvRange kv_plan(const KvAttendArgs &a, int find)
     r.live = r.splits = r.first = 0;
     return r;
 }
+
+// what a block's products are multiplied by, its key scale times the softmax scale: neither 0, which masked places (-inf) turn into not a number, nor
+// infinite, which products of 0 do
+__device__ __forceinline__ float logit_factor(float key_scale, float scale2) { return __builtin_amdgcn_fmed3f(key_scale * scale2, 0x1p-149f, 3.402823466e38f); }
 
 __device__ __forceinline__ float row_max(float x)
 {
@@ -738,7 +742,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
     }
     for (int u = 0; u < many; ++u) {
         const int j = __builtin_amdgcn_readlane(js, u & 63);
-        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[0]), u & 63)) * a.scale2;
+        const float ks = logit_factor(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[0]), u & 63)), a.scale2);
         float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[1]), u & 63));
         if ((u & 63) == 63) look(u + 1);
         const int pn = u + 1 < many ? __builtin_amdgcn_readlane(ps, (u + 1) & 63) : -1;
@@ -1047,7 +1051,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
                     s[t] = T::mfma(bring8<T>(w.z, w.w, 1.f), q[2 * i + 1], s[t]);
                 }
             }
-            softmax(s, ks * a.scale2, j, (j + 1) * KB <= wleast);
+            softmax(s, logit_factor(ks, a.scale2), j, (j + 1) * KB <= wleast);
             typename T::x8 p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = pack(s[i / 2], i % 2);

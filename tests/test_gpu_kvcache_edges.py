@@ -168,3 +168,22 @@ def test_values_of_fp16_at_both_ends(D, n, lens, size):
     check_tight(want, ctx.kv_attend(cache, q.cuda()), HF, below, "ends")
     lists = torch.arange(c["table"].shape[2], dtype=torch.int32).expand(B, n, H, -1).contiguous()
     check_tight(want, ctx.kv_attend(cache, q.cuda(), lists=lists.cuda()), HF, 2.0 ** -39, "ends, listed")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,size,scale,qsize", [(1, 2.0 ** -12, 1e-44, 1.0), (90, 2.0 ** -12, 1e-44, 1.0), (1, 2.0 ** 10, 3e38, 0.0), (90, 2.0 ** 10, 3e38, 0.0)])
+def test_logits_whose_factor_leaves_float32(dtype, n, size, scale, qsize):
+    """The softmax scale times a block's key scale is less than float32's smallest number, or more than its largest: every logit is zero (nearly, or for
+    queries of zeros), and a row's output is the mean of what it sees."""
+    say("factors", dtype, n, size, scale)
+    D, H, g, lens = 64, 1, 2, [300, 150]
+    rand = torch.Generator().manual_seed(n)
+    c = kv.new_cache(2, H, D, 5, dtype)
+    k, v = (size * (torch.rand(2, 300, H, D, generator=rand) + 0.5)).to(dtype), torch.randn(2, 300, H, D, generator=rand).to(dtype)
+    kv.append(c, k, v, torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    q = queries(rand, dtype, 2, n, H * g, D, qsize)
+    lse = torch.empty(q.shape[:3], device="cuda")
+    mass = torch.empty(c["table"].shape, device="cuda")
+    out = context().kv_attend(on_gpu(c), q.cuda(), scale=scale, lse=lse, mass_out=mass)
+    check_out(kv.attend(c, q, scale), out, dtype, "factors", lse, mass)
