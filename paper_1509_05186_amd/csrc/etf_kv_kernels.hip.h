@@ -992,9 +992,20 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = reference<T::TILE_UP>(fmaxf(top, __shfl_xor(top, 32)) * scale);
+        top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+        // z is s * scale less the reference with one rounding, as long as what rounding the largest z has left out matters no more than the others'
+        // roundings; from there on, with one more, no z is above the largest: exponentials stay within the type
+        if (__any(fabsf(top) > 0x1p20f)) {
+            asm volatile("");  // a branch: few blocks need it
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] *= scale;
+            scale = 1.f;
+        }
+        top = reference<T::TILE_UP>(top);
         // the reference in use may lag behind by a factor of 2^TILE_LAG in the weights, which changes nothing but spares the scaling
-        if (__any(top > m + T::TILE_LAG)) {
+        if (__any(top - m > T::TILE_LAG)) {
             const float was = m;
             m = fmaxf(m, top);
             const float fade = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(was - m);

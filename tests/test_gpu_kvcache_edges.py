@@ -187,3 +187,27 @@ def test_logits_whose_factor_leaves_float32(dtype, n, size, scale, qsize):
     mass = torch.empty(c["table"].shape, device="cuda")
     out = context().kv_attend(on_gpu(c), q.cuda(), scale=scale, lse=lse, mass_out=mass)
     check_out(kv.attend(c, q, scale), out, dtype, "factors", lse, mass)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,sign", [(1, 1), (90, 1), (90, -1), (120, 1)])
+def test_logits_larger_than_float32_resolves(dtype, n, sign):
+    """Logits of up to 2^38 (bf16) and 2^30 (fp16), steps of 2^14 and 2^6 between neighbouring float32 numbers: the largest ones, which equal each other exactly, share the weight."""
+    say("large logits", dtype, n, sign)
+    D, lens = 64, [400, 200]
+    rand = torch.Generator().manual_seed(n)
+    c = kv.new_cache(2, 1, D, 7, dtype)
+    k, v, t = torch.zeros(2, 400, 1, D), torch.randn(2, 400, 1, D, generator=rand), torch.arange(400)
+    k[..., 0] = (sign * 1.375 * torch.exp2(8.0 + t % 7))[None, :, None]
+    kv.append(c, k.to(dtype), v.to(dtype), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    q = torch.zeros(2, n, 1, D)
+    q[..., 0] = ((1 + torch.arange(n) % 127 / 128) * 2.0 ** (15 if dtype == HF else 23))[:, None]
+    q = q.to(dtype)
+    want = kv.attend(c, q, 1.0)
+    lse = torch.empty(2, n, 1, device="cuda")
+    out = context().kv_attend(on_gpu(c), q.cuda(), scale=1.0, lse=lse).double().cpu()
+    u, e = torch.finfo(dtype).eps / 2, 2.0 ** -24
+    tol = (u + 2 * e * want["seen"][..., None]) * want["size"] + u * want["out"].abs() + (2.0 ** -31 * (want["seen"] * want["vmax"])[..., None] + 2.0 ** -25 if dtype == HF else 0)
+    assert ((out - want["out"]).abs() <= tol).all()
+    assert ((lse.double().cpu() - want["lse"]).abs() <= 8 * e * want["lse"].abs()).all()
