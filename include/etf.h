@@ -529,7 +529,7 @@ int etf_ivf_search(etf_ctx *ctx, const float *queries, int64_t Q, int k, int w, 
  * (i32 [batch], device; NULL: all n) is how many of the n tokens each sequence has, the first ones.  Query head x
  * reads key/value head x / (heads_q / heads).
  * Query token i of a sequence is token lens - counts + i of its cache and sees the tokens up to itself.  Padding
- * and tokens that see nothing get zeros and a logarithm of -inf. */
+ * and tokens that see nothing get zeros and a logarithm of -inf; the others become not a number where the query is not finite. */
 #define ETF_KV_BLOCK 64      /* tokens of a block */
 #define ETF_KV_MAX_LIST 4096 /* largest w */
 enum { ETF_KV_BF16 = 0, ETF_KV_FP16 = 1 };  /* type of queries, new tokens, outputs and open blocks */

@@ -128,6 +128,15 @@ __device__ __forceinline__ uint32_t size8(const uint4 &w)
     return max((uint32_t)m[0], (uint32_t)m[1]);
 }
 
+// A piece of a query: one that is not finite is made NaN, so that its row becomes not a number even where all products would be -inf
+template <typename T>
+__device__ __forceinline__ typename T::x8 query8(typename T::x8 q)
+{
+    uint4 w = __builtin_bit_cast(uint4, q);
+    if (size8(w) >= T::EXP) w.x = T::NOT | (uint32_t)T::NOT << 16;
+    return __builtin_bit_cast(typename T::x8, w);
+}
+
 // Codes in the order of their values, two to a word: 16-bit numbers whose low byte is the code, its lower bits turned where it is
 // negative (so that -0 stands below +0).  Its own inverse.
 __device__ __forceinline__ i16x2 code_order(i16x2 code) { return code ^ ((code >> 15) & (int16_t)0x7F); }
@@ -740,6 +749,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
         load_k(page);
         load_v(page);
     }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[ks] = query8<T>(q[ks]);  // behind the first block's loads
     for (int u = 0; u < many; ++u) {
         const int j = __builtin_amdgcn_readlane(js, u & 63);
         const float ks = logit_factor(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ss[0]), u & 63)), a.scale2);
@@ -943,7 +954,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
     for (int i = 0; i < 2 * PAIRS; ++i) {
         uint4 w = make_uint4(0, 0, 0, 0);
         if (live) w = *reinterpret_cast<const uint4 *>(qp + 16 * (i / 2 * 2 + half) + 8 * (i % 2));
-        q[i] = __builtin_bit_cast(typename T::x8, w);
+        q[i] = query8<T>(__builtin_bit_cast(typename T::x8, w));
     }
     f32x16 o[DT];
 #pragma unroll

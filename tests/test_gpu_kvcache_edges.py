@@ -211,3 +211,30 @@ def test_logits_larger_than_float32_resolves(dtype, n, sign):
     tol = (u + 2 * e * want["seen"][..., None]) * want["size"] + u * want["out"].abs() + (2.0 ** -31 * (want["seen"] * want["vmax"])[..., None] + 2.0 ** -25 if dtype == HF else 0)
     assert ((out - want["out"]).abs() <= tol).all()
     assert ((lse.double().cpu() - want["lse"]).abs() <= 8 * e * want["lse"].abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,g", [(2, 4), (90, 2)])
+def test_an_infinite_query_makes_its_row_not_a_number(dtype, n, g):
+    """Also where every product is -inf, which is no row that sees nothing; and a row that sees nothing stays one."""
+    say("infinite queries", dtype, n, g)
+    D, H, lens = 64, 1, [300, n + 30]
+    rand = torch.Generator().manual_seed(n)
+    c = kv.new_cache(2, H, D, 5, dtype)
+    k, v = torch.randn(2, 300, H, D, generator=rand), torch.randn(2, 300, H, D, generator=rand)
+    k[..., 5], k[..., 6] = -k[..., 5].abs() - 1, k[..., 6].abs() + 1
+    kv.append(c, k.to(dtype), v.to(dtype), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    q = queries(rand, dtype, 2, n, H * g, D)
+    cnt = torch.tensor([n, n - 1], dtype=torch.int32)
+    want = kv.attend(c, q, 0.125, cnt)
+    lse, bad = torch.empty(q.shape[:3], device="cuda"), q.clone()
+    bad[0, 0, 1, 5], bad[0, 1, 0, 6], bad[1, 0, 0, 5], bad[1, n - 1, 1, 5] = float("inf"), -float("inf"), float("inf"), float("inf")     # the last one is padding
+    rows = [(0, 0, 1), (0, 1, 0)] + [(1, 0, 0)]
+    lists = torch.arange(5, dtype=torch.int32).expand(2, n, H, -1).contiguous().cuda()
+    for some in (None, lists):
+        out = context().kv_attend(on_gpu(c), bad.cuda(), scale=0.125, counts=cnt.cuda(), lists=some, lse=lse)
+        for row in rows:
+            assert torch.isnan(out[row].float()).all() and torch.isnan(lse[row])
+            out[row], lse[row] = want["out"][row].to(dtype).cuda(), float(want["lse"][row])
+        check_out(want, out, dtype, "the others", lse)
