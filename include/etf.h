@@ -520,9 +520,11 @@ int etf_ivf_search(etf_ctx *ctx, const float *queries, int64_t Q, int k, int w, 
  *   lens    i32 [batch]                              tokens in each sequence's cache, the same for all its heads; counts as 0
  *                                                    below that and as 64 max_blocks + 63 above that
  *   evicted i32 [batch]                              blocks that etf_kv_evict has taken out of each sequence so far
- * A page belongs to one block of one head.  batch * heads * max_blocks < 2^31, and a call that needs a launch of 2^32 threads
- * or more is refused; head_dim is 64, 96 or 128; all arrays 16-byte aligned.  lens is advanced by the caller (after etf_kv_append, before etf_kv_attend with the new tokens'
- * queries); it may be taken back to no less than what the full blocks hold.
+ * A page belongs to one block of one head.  batch * heads * max_blocks < 2^31, and a call that needs a launch of 2^32
+ * threads or more is refused; head_dim is 64, 96 or 128; all arrays 16-byte aligned.  lens is advanced by the caller (after
+ * etf_kv_append, before etf_kv_attend with the new tokens' queries); it may be taken back to no less than what the full
+ * blocks hold.  Where an append has completed one block, the last so far, it may also be taken back to what it was before
+ * that append: those of its tokens that are to stay are then appended again (a draft of which some were rejected).
  *
  * Rows of k, v and q ([batch][n][heads or heads_q][head_dim], 16-bit) lie at strides[0..2] = elements from one sequence,
  * token and head to the next, multiples of 8 (a NULL pointer: dense); a row is contiguous and 16-byte aligned.  counts

@@ -238,3 +238,46 @@ def test_an_infinite_query_makes_its_row_not_a_number(dtype, n, g):
             assert torch.isnan(out[row].float()).all() and torch.isnan(lse[row])
             out[row], lse[row] = want["out"][row].to(dtype).cuda(), float(want["lse"][row])
         check_out(want, out, dtype, "the others", lse)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 96)])
+@pytest.mark.parametrize("length,draft,accepted", [(62, 4, 1), (62, 4, 3), (63, 1, 0), (126, 4, 2), (100, 60, 27), (100, 60, 28), (1, 120, 5)])
+def test_drafts_rejected_across_a_blocks_end(dtype, D, length, draft, accepted):
+    """A draft that completed a block is taken back to the length before it, and the accepted tokens are appended again: the cache goes on as if no other
+    had come."""
+    say("drafts", dtype, D, length, draft, accepted)
+    H, B, total = 2, 1, 300
+    g = torch.Generator().manual_seed(length + draft)
+    k, v = (torch.randn(B, total, H, D, generator=g).to(dtype).cuda() for _ in range(2))
+    other = [torch.randn(B, draft, H, D, generator=g).to(dtype).cuda() for _ in range(2)]
+    q = queries(g, dtype, B, 1, 2 * H, D).cuda()
+    plain, drafted = (etf.KvCache.alloc(B, H, D, total, dtype=dtype) for _ in range(2))
+    ctx = context()
+
+    def come(cache, first, last):
+        if last > first:
+            ctx.kv_append(cache, k[:, first:last], v[:, first:last])
+            cache.lens += last - first
+
+    for cache in (plain, drafted):
+        come(cache, 0, length)
+    for x, own in zip(other, (k, v)):
+        x[:, :accepted] = own[:, length : length + accepted]
+    ctx.kv_append(drafted, *other)
+    drafted.lens += draft
+    ctx.kv_attend(drafted, q)                   # the draft is looked at
+    drafted.lens -= draft
+    end = length + accepted
+    for cache in (plain, drafted):
+        come(cache, length, end)
+    assert torch.equal(ctx.kv_attend(drafted, q), ctx.kv_attend(plain, q))
+    come(plain, end, total)
+    for i in range(end, total, 50):
+        come(drafted, i, min(total, i + 50))
+        if i == end:
+            assert torch.isfinite(ctx.kv_attend(drafted, q).float()).all()
+    assert torch.equal(ctx.kv_attend(drafted, q), ctx.kv_attend(plain, q))
+    full = total // 64
+    for name in ("k", "v", "bounds", "scales"):
+        x, y = (getattr(c, name)[c.table[:, :, :full].long()] for c in (plain, drafted))
+        assert torch.equal(x.view(torch.uint8) if name != "scales" else x, y.view(torch.uint8) if name != "scales" else y)
