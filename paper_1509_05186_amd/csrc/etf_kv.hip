@@ -123,9 +123,11 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         // up to KV_ROUNDS rounds of workgroups (kv_plan) and one for each unit of a sequence; a card full of workgroups from the tiles of prompts alone
         // needs no ranges
         const int64_t units = c->batch * p.units;
-        // Short tables are no faster in ranges, which cost the join's launch.  Single tokens, 8 heads, in a graph: one sequence of 500
-        // tokens 8.6 us without and 10.3 with ranges, 1000 tokens 11.3 and 10.4 (but 14 and 16.5 called one by one), 2000 tokens 16.8
-        // and 10.4; 16 sequences of 1000 tokens 13.2 and 18.3, 2000 tokens 19.4 and 22.6, 4000 tokens 30.1 and 31.7.
+        // Short tables are hardly faster in ranges, whose join is a launch of its own; the host knows the table's columns but not the
+        // lengths, so a short sequence in a wide table is cut all the same.  Single tokens, 8 heads of 128 dimensions, not cut and cut: one sequence of 500
+        // tokens 9.1 and 11.4 us, 1000 tokens 11.7 and 11.4, 2000 tokens 16.8 and 11.5; 16 sequences of 1000 tokens 14.2 and 18.8, 2000 tokens
+        // 19.8 and 23.5, 4000 tokens 30.1 and 31.7.  From there on ragged lengths need the ranges, so the limit for many units stays below what
+        // equal lengths would allow.
         p.split = p.many ? units < 1024 : c->max_blocks > (units >= 128 ? 32 : 16);
         p.grid = (p.split ? KV_ROUNDS * KV_ROUND : 0) + units;
     }

@@ -353,7 +353,9 @@ struct KvAttendArgs {
 };
 
 constexpr int KV_LEAST = 4;    // blocks of a range, one to a wave
-constexpr int KV_ROUND = 512;  // workgroups that the card holds at once
+// Workgroups that the card holds at once: two to a compute unit, as many as 128 dimensions leave room for (64 KB of LDS in k_kv_attend, registers in
+// k_kv_tile).  The same number is planned with for 64 and 96 dimensions, of which more would fit.
+constexpr int KV_ROUND = 512;
 constexpr int KV_ROUNDS = 3;   // most rounds of them that ranges are made for
 
 // A sequence's workgroups: `live` tiles of `tiles` have rows that are no padding; first the ranges of those, heads innermost, then one to
@@ -736,6 +738,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
             if (hq == 0 && valid) a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = base + __builtin_amdgcn_logf(all_sum);
         }
     };
+    // The matrix cores' second operand has 16 bits: a weight is rounded to the type, off by half a unit of it at most, while its sum is
+    // not.  Two operands for each weight would keep 32 bits and double the second product.
     auto pack = [&](const f32x4 (&s)[4], int e) {
         const typename T::x2 p0 = T::narrow(s[2 * e][0], s[2 * e][1]), p1 = T::narrow(s[2 * e][2], s[2 * e][3]);
         const typename T::x2 p2 = T::narrow(s[2 * e + 1][0], s[2 * e + 1][1]), p3 = T::narrow(s[2 * e + 1][2], s[2 * e + 1][3]);
@@ -1039,7 +1043,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
             if (half == 0 && valid) a.block_lse[(bh * (a.c.blocks + 1) + j) * a.n * g + row] = base + __builtin_amdgcn_logf(sum);
         }
     };
-    // operand p^T of step u of tile t
+    // operand p^T of step u of tile t, rounded to the type as in k_kv_attend
     auto pack = [&](const f32x16 &s, int u) {
         const typename T::x2 p0 = T::narrow(s[8 * u], s[8 * u + 1]), p1 = T::narrow(s[8 * u + 2], s[8 * u + 3]);
         const typename T::x2 p2 = T::narrow(s[8 * u + 4], s[8 * u + 5]), p3 = T::narrow(s[8 * u + 6], s[8 * u + 7]);
