@@ -332,7 +332,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
 // 10.7 instead of 13.2 TB/s from the second-level cache); the next block's keys are asked for as soon as this one's are in
 // registers, the values likewise, so that a wave always has a block on its way.  A wave takes every fourth block of its workgroup's
 // range; the four join through LDS, ranges of a long cache through memory (k_kv_join).
-// Bound by memory: 820 MB of cache (four sequences of 100 000 tokens) at 5.5 TB/s, 545 MB (64 sequences of up to 8192) at 5.0; listed blocks of
+// Bound by memory: 820 MB of cache (four sequences of 100 000 tokens) at 5.5 TB/s, 545 MB (64 sequences of up to 8192) at 4.9; listed blocks of
 // many tokens by the second-level caches, 14.6 TB/s.
 // ------------------------------------------------------------------------------------------------
 struct KvAttendArgs {
@@ -911,8 +911,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a)
 // row and p^T stands in its registers as the second product wants it: row m of a tile of s^T is token
 // 16 (m / 4 % 2) + 8 (m / 16) + 4 (m / 8 % 2) + m % 4 of its 32.  The next block is on its way from memory to registers while this one
 // is worked on.  Pieces of 16 bytes are exchanged within a row of LDS, so that eight lanes that read together hit all banks.
-// Bound by vector issue beside the matrix cores (64 % and 42 % of the time): two prompts of 4096 tokens, 32 heads of 128 dimensions 302 us =
-// 910 TFLOP/s.  Making operands of the codes once a workgroup, on their way into LDS, instead of in every wave: 306 us.
+// Bound by vector issue beside the matrix cores (64 % and 42 % of the time): two prompts of 4096 tokens, 32 heads of 128 dimensions 302
+// to 332 us from card to card = 830 to 910 TFLOP/s.  Making operands of the codes once a workgroup, on their way into LDS, instead of in every wave: 306 us
+// where that is 302.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int D, bool MASS>
 __global__ __launch_bounds__(256, 2) void k_kv_tile(KvAttendArgs a)
