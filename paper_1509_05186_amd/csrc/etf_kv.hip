@@ -125,9 +125,9 @@ AttendPlan plan_attend(const etf_kv_cache *c, int n, int heads_q, int w, bool ma
         const int64_t units = c->batch * p.units;
         // Short tables are hardly faster in ranges, whose join is a launch of its own; the host knows the table's columns but not the
         // lengths, so a short sequence in a wide table is cut all the same.  Single tokens, 8 heads of 128 dimensions, not cut and cut: one sequence of 500
-        // tokens 9.1 and 11.4 us, 1000 tokens 11.7 and 11.4, 2000 tokens 16.8 and 11.5; 16 sequences of 1000 tokens 14.2 and 18.8, 2000 tokens
-        // 19.8 and 23.5, 4000 tokens 30.1 and 31.7.  From there on ragged lengths need the ranges, so the limit for many units stays below what
-        // equal lengths would allow.
+        // tokens 8.9 and 11.5 us, 1000 tokens 11.5 and 11.2, 2000 tokens 17.0 and 11.6; 16 sequences of 1000 tokens 14.2 and 18.8, 2000 tokens
+        // 19.8 and 23.3, 4000 tokens 30.5 and 32.0, but ragged ones 28.7 and 14.9 (one of 4000, the others of 500) and 29.9 and 23.8 (500 to 4000 evenly),
+        // so that the limit for many units stays below what equal lengths would allow.
         p.split = p.many ? units < 1024 : c->max_blocks > (units >= 128 ? 32 : 16);
         p.grid = (p.split ? KV_ROUNDS * KV_ROUND : 0) + units;
     }
