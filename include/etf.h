@@ -582,6 +582,28 @@ int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const 
 int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
                  int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
 
+/* ---- attention over whole prompts ---------------------------------------- */
+
+/* Causal attention of prompts that lie packed, one after the other, in 16 bits (etf_kv_append_packed takes the same keys and values
+ * into the cache): tokens [starts[b], starts[b + 1]) are sequence b's, and each sees its sequence's tokens up to itself.  With
+ * s = scale * <q, k_t>: out = sum softmax(s)_t v_t, lse = log sum exp(s).  Sums, maxima and products are float32; weights are
+ * rounded to the rows' type for their product with the values.
+ *   dtype, head_dim   ETF_KV_BF16 or ETF_KV_FP16; 64, 96 or 128
+ *   q       16-bit [tokens][heads_q][head_dim]; k, v [tokens][heads][head_dim].  Rows lie at strides[0..1] = elements from one token
+ *           and head to the next, multiples of 8, of tokens up to 2^23 (a NULL pointer: dense); a row is contiguous and 16-byte
+ *           aligned.  Query head x reads key/value head x / (heads_q / heads)
+ *   starts  i32 [batch + 1], device, ascending, within [0, tokens]; counts as 0 or as tokens outside of that.  A sequence of no tokens, or
+ *           whose end lies before its start, has no rows
+ *   out     dense [tokens][heads_q][head_dim], the rows' type; lse: NULL or float [tokens][heads_q].  Rows of tokens that
+ *           are no sequence's are left as they were
+ *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes
+ * A row whose query, or of which a key that it sees, makes a logit +inf or not a number becomes not a number; a value that is not finite
+ * makes its dimension so, in the rows that see it and in no other. */
+int64_t etf_prompt_attend_workspace_bytes(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch);
+int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const void *q, const int64_t *q_strides, const void *k, const int64_t *k_strides, const void *v,
+                      const int64_t *v_strides, int64_t tokens, int heads_q, int heads, const int32_t *starts, int batch, float scale, void *out, float *lse,
+                      void *ws, int64_t ws_bytes);
+
 /* ---- per-kernel timing (for benchmarks) ---------------------------------- */
 
 /* Kernel classes of the hot path, in launch order. */

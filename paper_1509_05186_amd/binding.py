@@ -29,6 +29,7 @@ EXPORTS = [
     "etf_ivf_set_coarse", "etf_ivf_assign_workspace_bytes", "etf_ivf_assign_device", "etf_ivf_build", "etf_ivf_stats",
     "etf_ivf_device_bytes", "etf_ivf_upload", "etf_ivf_workspace_bytes", "etf_ivf_search",
     "etf_kv_append", "etf_kv_attend_workspace_bytes", "etf_kv_attend", "etf_kv_select_workspace_bytes", "etf_kv_select", "etf_kv_evict",
+    "etf_prompt_attend_workspace_bytes", "etf_prompt_attend",
 ]
 ETF_BUILD_NONE, ETF_BUILD_CHAIN, ETF_BUILD_GENERAL, ETF_BUILD_GENERAL_AFTER_CHAIN = 0, 1, 2, 3
 ETF_PROBE_READ, ETF_PROBE_WRITE, ETF_PROBE_COPY, ETF_PROBE_ROWS, ETF_PROBE_LDS, ETF_PROBE_LDS_SCATTER = 0, 1, 2, 3, 4, 5
@@ -193,6 +194,8 @@ def load_library():
         "etf_kv_select_workspace_bytes": (L, [P, P, I, I, I]),
         "etf_kv_select": (I, [P, P, P, P, I, I, P, I, I, I, P, P, L]),
         "etf_kv_evict": (I, [P, P, P, I, I, I, P, P, P, P, P]),
+        "etf_prompt_attend_workspace_bytes": (L, [P, I, L, I, I, I]),
+        "etf_prompt_attend": (I, [P, I, I, P, P, P, P, P, P, L, I, I, P, I, ctypes.c_float, P, P, P, L]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -842,6 +845,75 @@ class Context:
         c = (cache if to is None else to)._c
         self._ck(self._lib.etf_kv_evict(self._h, cache._ref, pm, budget, sink, recent, c.table, c.lens, c.evicted, po, pf))
         return mass_out, freed
+
+    # ---- attention over whole prompts
+    def _here(self, gpu: int, device):
+        if gpu != self._device and self._device is not None:
+            raise ValueError("the tensors are on %s, the context on GPU %d" % (device, self._device))
+
+    def _empty(self, gpu: int, like, shape, dtype):
+        """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
+        import torch
+        mine = self._stream or 0
+        if gpu < 0 or _current_stream(gpu) == mine:
+            return torch.empty(shape, dtype=dtype, device=like.device)
+        # torch takes a stream of its pool for a pointer of zero
+        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=like.device) if mine else torch.cuda.default_stream(like.device)):
+            return torch.empty(shape, dtype=dtype, device=like.device)
+
+    @staticmethod
+    def _packed(t, tokens, heads, dim, like, what: str):
+        """(pointer, strides) of rows [tokens][heads][dim]; dense ones need no strides."""
+        if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or t.shape[2] != dim or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads):
+            raise ValueError("%s: expected a %s tensor [%d][%s][%d] on %s" % (what, like.dtype, tokens, "heads" if heads is None else heads, dim, like.device))
+        if t.is_contiguous():
+            return t.data_ptr(), None
+        s = t.stride()
+        if s[2] != 1:
+            raise ValueError("%s: a row's elements must be contiguous" % what)
+        # of a dimension of one torch allows any stride, which nothing uses
+        return t.data_ptr(), (ctypes.c_int64 * 2)(*(s[i] if t.shape[i] > 1 else 0 for i in range(2)))
+
+    @staticmethod
+    def _plain(t, shape, dtype, like, what: str):
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
+            raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (what, dtype, list(shape), like.device))
+        return t.data_ptr()
+
+    def prompt_attend_workspace_bytes(self, tokens: int, heads_q: int, heads: int, head_dim: int, batch: int) -> int:
+        return self._ck(self._lib.etf_prompt_attend_workspace_bytes(self._h, head_dim, tokens, heads_q, heads, batch))
+
+    def prompt_attend(self, q, k, v, starts, scale: Optional[float] = None, out=None, lse=None, ws=None):
+        """Causal attention of packed prompts: q [tokens][heads_q][D], k, v [tokens][heads][D], bfloat16 or float16; sequence b has the tokens
+        [starts[b], starts[b + 1]), starts int32 [B + 1].  scale: 1 / sqrt(D) by default; lse: float32 [tokens][heads_q], written if given.
+        Rows of tokens that are no sequence's are left as they were.  There is no gradient: tensors that require one are refused
+        where torch would record it."""
+        import torch
+        for t, what in ((q, "q"), (k, "k"), (v, "v")):
+            self._no_gradient(t, what)
+        if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("expected q [tokens][heads_q][D] and k [tokens][heads][D], bfloat16 or float16")
+        (tokens, heads_q, D), heads, gpu = q.shape, k.shape[1], q.get_device()
+        self._here(gpu, q.device)
+        pq, sq = self._packed(q, tokens, None, D, q, "q")
+        pk, sk = self._packed(k, tokens, heads, D, q, "k")
+        pv, sv = self._packed(v, tokens, heads, D, q, "v")
+        if starts.dim() != 1 or starts.shape[0] < 2:
+            raise ValueError("starts: expected a tensor [B + 1], B at least 1")
+        batch = starts.shape[0] - 1
+        ps = self._plain(starts, (batch + 1,), torch.int32, q, "starts")
+        if out is None:
+            out = self._empty(gpu, q, q.shape, q.dtype)
+        po = self._plain(out, q.shape, q.dtype, q, "out")
+        pe = self._plain(lse, (tokens, heads_q), torch.float32, q, "lse")
+        if ws is None:
+            ws = self._empty(gpu, q, (self.prompt_attend_workspace_bytes(tokens, heads_q, heads, D, batch) + 256,), torch.uint8)
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_prompt_attend(self._h, ETF_KV_BF16 if q.dtype == torch.bfloat16 else ETF_KV_FP16, D, pq, sq, pk, sk, pv, sv, tokens, heads_q, heads,
+                                             ps, batch, D ** -0.5 if scale is None else scale, po, pe, pw, nw))
+        return out
 
     def probe_bandwidth(self, kind: int, a, b, nbytes: int):
         """One launch of a streaming probe kernel over the uint8 device tensors a and b (256-byte aligned)."""

@@ -1,0 +1,102 @@
+// Attention over whole prompts: checks of arguments, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <limits>
+
+#include "etf_internal.h"
+#include "etf_launch.h"
+
+using namespace etf;
+
+namespace {
+
+#include "etf_prompt_kernels.hip.h"
+
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// strides of token and head of rows [tokens][heads][dim]
+int check_packed(const etf_ctx *ctx, const char *what, const void *p, const int64_t *strides, int64_t heads, int dim, int64_t (&out)[2])
+{
+    if (!p || !aligned16(p)) return fail(ctx, ETF_EINVAL, "%s is null or not 16-byte aligned", what);
+    out[0] = strides ? strides[0] : heads * dim;
+    out[1] = strides ? strides[1] : dim;
+    for (int i = 0; i < 2; ++i)
+        if (out[i] < 0 || out[i] % 8 != 0 || out[i] > (i ? (int64_t)1 << 40 : (int64_t)1 << 23))
+            return fail(ctx, ETF_EINVAL, "stride %d of %s must be a multiple of 8 elements, not negative and within bounds (it is %lld)", i, what, (long long)out[i]);
+    return ETF_OK;
+}
+
+struct PromptPlan {
+    int64_t tiles = 0, grid = 0, total = 256;
+};
+
+int plan_prompt(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch, PromptPlan &p)
+{
+    if (!ctx) return ETF_EINVAL;
+    if (head_dim != 64 && head_dim != 96 && head_dim != 128) return fail(ctx, ETF_EINVAL, "head_dim must be 64, 96 or 128 (it is %d)", head_dim);
+    if (tokens < 1 || heads_q < 1 || heads < 1 || batch < 1)
+        return fail(ctx, ETF_EINVAL, "tokens, heads_q, heads and batch must be positive (%lld, %d, %d, %d)", (long long)tokens, heads_q, heads, batch);
+    if (heads_q % heads != 0) return fail(ctx, ETF_EINVAL, "heads_q (%d) must be a multiple of heads (%d)", heads_q, heads);
+    if (tokens > INT32_MAX / heads_q || batch > (1 << 24)) return fail(ctx, ETF_EINVAL, "tokens * heads_q must stay below 2^31, batch up to 2^24");
+    p.tiles = tokens * (heads_q / heads) / 128 + batch;
+    p.grid = p.tiles * heads;
+    if (p.grid > (int64_t)UINT32_MAX / 256) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    return ETF_OK;
+}
+
+template <typename T, int D>
+int launch_prompt(etf_ctx *ctx, const PromptArgs &a, const PromptPlan &p)
+{
+    ProfScope prof(ctx, ETF_K_KV);
+    hipLaunchKernelGGL((k_prompt<T, D>), dim3((unsigned)p.grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+    LAUNCH_CHECK(ctx, "k_prompt");
+    return ETF_OK;
+}
+template <typename T>
+int launch_prompt(etf_ctx *ctx, const PromptArgs &a, const PromptPlan &p, int head_dim)
+{
+    return head_dim == 64 ? launch_prompt<T, 64>(ctx, a, p) : head_dim == 96 ? launch_prompt<T, 96>(ctx, a, p) : launch_prompt<T, 128>(ctx, a, p);
+}
+
+}  // namespace
+
+extern "C" int64_t etf_prompt_attend_workspace_bytes(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch)
+{
+    PromptPlan p;
+    const int rc = plan_prompt(ctx, head_dim, tokens, heads_q, heads, batch, p);
+    return rc != ETF_OK ? rc : p.total;
+}
+
+extern "C" int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const void *q, const int64_t *q_strides, const void *k, const int64_t *k_strides,
+                                 const void *v, const int64_t *v_strides, int64_t tokens, int heads_q, int heads, const int32_t *starts, int batch, float scale,
+                                 void *out, float *lse, void *ws, int64_t ws_bytes)
+{
+    PromptPlan p;
+    int rc = plan_prompt(ctx, head_dim, tokens, heads_q, heads, batch, p);
+    if (rc != ETF_OK) return rc;
+    if (dtype != ETF_KV_BF16 && dtype != ETF_KV_FP16) return fail(ctx, ETF_EINVAL, "unknown type %d", dtype);
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, ETF_EINVAL, "scale must be positive and finite");
+    if (!starts || !out || !aligned16(out)) return fail(ctx, ETF_EINVAL, "starts or out is null, or out not 16-byte aligned");
+    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(ctx, ETF_EINVAL, "workspace is null or not 256-byte aligned");
+    if (ws_bytes < p.total) return fail(ctx, ETF_ENOMEM, "workspace too small: %lld < %lld", (long long)ws_bytes, (long long)p.total);
+    PromptArgs a{};
+    if ((rc = check_packed(ctx, "q", q, q_strides, heads_q, head_dim, a.qs)) != ETF_OK) return rc;
+    if ((rc = check_packed(ctx, "k", k, k_strides, heads, head_dim, a.ks)) != ETF_OK) return rc;
+    if ((rc = check_packed(ctx, "v", v, v_strides, heads, head_dim, a.vs)) != ETF_OK) return rc;
+    a.q = (const uint16_t *)q;
+    a.k = (const uint16_t *)k;
+    a.v = (const uint16_t *)v;
+    a.starts = starts;
+    a.out = (uint16_t *)out;
+    a.lse = lse;
+    a.scale2 = std::min(scale * 1.4426950408889634f, std::numeric_limits<float>::max());
+    a.tokens = (int)tokens;
+    a.batch = batch;
+    a.heads = heads;
+    a.g = heads_q / heads;
+    if (ctx->device < 0) return fail(ctx, ETF_ENOGPU, "host-only context");
+    HIP_TRY(ctx, hipSetDevice(ctx->device));
+    return dtype == ETF_KV_BF16 ? launch_prompt<TBf>(ctx, a, p, head_dim) : launch_prompt<THf>(ctx, a, p, head_dim);
+}

@@ -1,0 +1,283 @@
+// Kernel of attention over whole prompts (etf_prompt_attend).  Included by etf_prompt.hip, inside its anonymous namespace.
+#pragma once
+
+#include "etf_kv_types.hip.h"
+
+struct PromptArgs {
+    const uint16_t *q, *k, *v;
+    int64_t qs[2], ks[2], vs[2];  // strides of token, head
+    const int32_t *starts;
+    uint16_t *out;
+    float *lse;
+    float scale2;  // softmax scale times log2 e, finite
+    int tokens, batch, heads, g;
+};
+
+// first token of sequence b (b = batch: the end of the last), within the tokens that there are
+__device__ __forceinline__ int prompt_start(const PromptArgs &a, int b) { return min(max(a.starts[b], 0), a.tokens); }
+
+// Sequences share one numbering of tiles that needs no counting: sequence b's tiles of ROWS rows begin at number floor(starts[b] g / ROWS) + b,
+// since it has at most floor(n g / ROWS) + 1 of them.  The last sequence that begins at or before `find`, by a search of
+// 64 places at a time.  Every lane of the wave calls it.
+template <int ROWS>
+__device__ __forceinline__ int prompt_of_tile(const PromptArgs &a, int find)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, many = a.batch;  // it is one of [lo, lo + many)
+    while (many > 1) {
+        const int step = (many + 63) / 64, i = lane * step;
+        const int b = lo + i;
+        const bool before = i < many && (int64_t)prompt_start(a, b) * a.g / ROWS + b <= find;
+        const uint64_t all = __ballot(before);
+        const int last = all ? 63 - __builtin_clzll(all) : 0;
+        lo += last * step;
+        many = min(step, many - last * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention of prompts in 16 bits.  Rows are pairs (token, query head of the group) of one sequence and key/value head, 128 to
+// a workgroup, 32 to a wave.  s^T = K q^T and o^T = V^T p^T on v_mfma_f32_32x32x16: a lane's column is a row, so the running
+// maximum and sum are the lane's own (and its neighbour's 32 lanes up), and p^T stands in its registers as the second product wants
+// it: of 16 tokens, those 8 (j / 4) + 4 (lane / 32) + j % 4.  Blocks of 64 tokens go straight from memory to LDS, the next one while this
+// one is worked on; values are read transposed (ds_read_b64_tr_b16: 16 lanes exchange 4 x 4 numbers).  Pieces of 16 bytes are
+// exchanged within a row of LDS, so that lanes that read together hit all banks.
+// ------------------------------------------------------------------------------------------------
+// 16 bytes to a lane from offset `at` of the `bytes` bytes at `from` (nothing is read behind them) to the 1 KB of LDS at `to`, in the
+// order of the lanes.  `from`, `bytes` and `to` are the same for all lanes.
+__device__ __forceinline__ void buffer_to_lds(const void *from, int bytes, uint32_t at, void *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)from, 0, bytes, 0x00020000), (__attribute__((address_space(3))) void *)to, 16, at, 0, 0, 0);
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int D>
+struct PromptTile {
+    static constexpr int PT = D / 8;  // pieces of a row
+    // place in its row of LDS of piece `at` of a token's keys, values; BACK: the piece that stands at place `at`
+    template <bool BACK>
+    static __device__ __forceinline__ int k_place(int token, int at)
+    {
+        if constexpr (D == 96) return (at + (BACK ? 12 - (token >> 2 & 7) : token >> 2 & 7)) % 12;
+        return at ^ (D == 128 ? token & 15 : token >> 1 & 7);
+    }
+    static __device__ __forceinline__ int v_place(int token, int at) { return at ^ (D == 128 ? (token & 3) << 2 : D == 64 ? (token >> 1 & 1) << 2 : 0); }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
+{
+    using Tile = PromptTile<D>;
+    constexpr int ROWS = 128, PT = Tile::PT, LOADS = PT / 4, DT = D / 32, ST = D / 16;
+    __shared__ __attribute__((aligned(1024))) uint8_t s_k0[KB * D * 2], s_v0[KB * D * 2], s_k1[KB * D * 2], s_v1[KB * D * 2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
+    const int H = a.heads, g = a.g;
+    const int h = blockIdx.x % H, find = (int)(gridDim.x / H) - 1 - (int)(blockIdx.x / H);  // a prompt's last tiles, the longest ones, first
+    const int b = prompt_of_tile<ROWS>(a, find);
+    const int begin = __builtin_amdgcn_readfirstlane(prompt_start(a, b)), n = __builtin_amdgcn_readfirstlane(prompt_start(a, b + 1)) - begin;
+    const int tile = __builtin_amdgcn_readfirstlane(find - (int)((int64_t)begin * g / ROWS) - b);
+    if (n <= 0 || tile < 0 || (int64_t)tile * ROWS >= (int64_t)n * g) return;
+    const int64_t rows = (int64_t)n * g, row0 = (int64_t)tile * ROWS, row = row0 + 32 * wave + x;
+    const bool valid = row < rows;
+    const int qi = (int)(min(row, rows - 1) / g), hg = valid ? (int)(row % g) : 0;
+    const int sees = qi + 1;
+    const int wleast = __builtin_amdgcn_readfirstlane(sees), wmost = __builtin_amdgcn_readfirstlane((int)(min(row0 + 32 * wave + 31, rows - 1) / g) + 1);
+    const bool wlive = row0 + 32 * wave < rows;
+    const int most = (int)(min(row0 + ROWS - 1, rows - 1) / g) + 1, blocks = (most + KB - 1) / KB;
+
+    typename T::x8 q[ST];
+    const uint16_t *qp = a.q + (begin + qi) * a.qs[0] + ((int64_t)h * g + hg) * a.qs[1];
+#pragma unroll
+    for (int i = 0; i < ST; ++i) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (valid) w = *reinterpret_cast<const uint4 *>(qp + 16 * i + 8 * half);
+        q[i] = query8<T>(__builtin_bit_cast(typename T::x8, w));
+    }
+
+    // where this lane's pieces of a block come from, in bytes from the block's first key or value
+    uint32_t k_from[LOADS], v_from[LOADS];
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) {
+        const int p = (wave * LOADS + l) * 64 + lane, t = p / PT, at = p % PT;
+        k_from[l] = t * (uint32_t)a.ks[0] * 2 + Tile::template k_place<true>(t, at) * 16;
+        v_from[l] = t * (uint32_t)a.vs[0] * 2 + Tile::v_place(t, at) * 16;
+    }
+    const uint16_t *kp = a.k + begin * a.ks[0] + h * a.ks[1], *vp = a.v + begin * a.vs[0] + h * a.vs[1];
+    auto load = [&](int j, uint8_t *to_k, uint8_t *to_v) __attribute__((always_inline)) {
+        const int last = min(KB, n - j * KB) - 1;  // rows behind the sequence's end are out of the buffers' range
+        const void *fk = kp + (int64_t)j * KB * a.ks[0], *fv = vp + (int64_t)j * KB * a.vs[0];
+        const int nk = last * (int)a.ks[0] * 2 + D * 2, nv = last * (int)a.vs[0] * 2 + D * 2;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) buffer_to_lds(fk, nk, k_from[l], to_k + (wave * LOADS + l) * 1024);
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) buffer_to_lds(fv, nv, v_from[l], to_v + (wave * LOADS + l) * 1024);
+    };
+
+    f32x16 o[DT];
+    float m, l;
+    const int l16 = lane & 15, quad = l16 >> 2;
+    const int v_at = (4 * half + quad) * D * 2 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;  // of the dimensions from 0 on, before exchange
+    // four tokens from 16 u + 8 c + 4 half on of dimension 32 i + x
+    auto value4 = [&](const uint8_t *s_v, int u, int c, int i) __attribute__((always_inline)) {
+        const int seg = D == 128 ? i ^ quad : D == 64 ? i ^ (quad >> 1) : i;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(s_v + v_at + seg * 64 + (16 * u + 8 * c) * D * 2));
+    };
+    auto value8 = [&](const uint8_t *s_v, int u, int i) __attribute__((always_inline)) {
+        const s16x4 v0 = value4(s_v, u, 0, i), v1 = value4(s_v, u, 1, i);
+        return (u32x4){__builtin_bit_cast(uint2, v0).x, __builtin_bit_cast(uint2, v0).y, __builtin_bit_cast(uint2, v1).x, __builtin_bit_cast(uint2, v1).y};
+    };
+
+    auto block = [&](auto careful, int j, const uint8_t *s_k, const uint8_t *s_v) __attribute__((always_inline)) {
+        f32x16 s[2];
+        s[0] = s[1] = (f32x16)(0.f);
+#pragma unroll
+        for (int i = 0; i < ST; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int at = (32 * t + x) * D * 2 + Tile::template k_place<false>(x, 2 * i + half) * 16;
+                s[t] = T::mfma(*reinterpret_cast<const typename T::x8 *>(s_k + at), q[i], s[t]);
+            }
+        float scale = a.scale2;
+        if (j * KB + KB > wleast) {
+            asm volatile("");  // a branch: few blocks need the comparisons
+            const int left = sees - j * KB - 4 * half;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (32 * t + 8 * (i / 4) + i % 4 >= left) s[t][i] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+        // z is s * scale less the reference with one rounding, as long as what rounding the largest z has left out matters no more than the others'
+        // roundings; from there on, with one more, no z is above the largest: exponentials stay within the type.  Here and below a row goes by
+        // its own numbers alone, so that its result does not depend on the rows beside it.
+        const bool far = fabsf(top) > 0x1p20f;
+        if (__any(far)) {
+            asm volatile("");  // a branch: few blocks need it
+            const float now = far ? scale : 1.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] *= now;
+            scale = far ? 1.f : scale;
+        }
+        top = reference<T::TILE_UP>(top);
+        // the reference in use may lag behind by a factor of 2^TILE_LAG in the weights, which changes nothing but spares the scaling
+        const bool more = top - m > T::TILE_LAG;
+        if (__any(more)) {
+            const float fade = more ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+            m = more ? top : m;
+            l *= fade;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] *= fade;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, -base));
+                sum += s[t][i];
+            }
+        l += sum;
+        typename T::x8 p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x16 &w = s[u / 2];
+            const int at = 8 * (u % 2);
+            const typename T::x2 p0 = T::narrow(w[at], w[at + 1]), p1 = T::narrow(w[at + 2], w[at + 3]);
+            const typename T::x2 p2 = T::narrow(w[at + 4], w[at + 5]), p3 = T::narrow(w[at + 6], w[at + 7]);
+            p[u] = (typename T::x8){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+        }
+        if constexpr (!decltype(careful)::value) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[i] = T::mfma(__builtin_bit_cast(typename T::x8, value8(s_v, u, i)), p[u], o[i]);
+        } else {
+            // values that are not finite go to the rows that see them, and to no other: zeros in the product, then added
+            uint32_t some = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    u32x4 w = value8(s_v, u, i);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t lo = (w[y] & T::EXP) == T::EXP ? 0xFFFFu : 0u, hi = (w[y] >> 16 & T::EXP) == T::EXP ? 0xFFFF0000u : 0u;
+                        some |= lo | hi;
+                        w[y] &= ~(lo | hi);
+                    }
+                    o[i] = T::mfma(__builtin_bit_cast(typename T::x8, w), p[u], o[i]);
+                }
+            if (!__any(some != 0)) return;
+#pragma unroll 1
+            for (int t = 0; t < min(KB, n - j * KB); ++t) {
+                const bool see = j * KB + t < sees;
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) {
+                        const int d = 32 * i + 8 * (y / 4) + 4 * half + y % 4;
+                        const uint16_t u = *reinterpret_cast<const uint16_t *>(s_v + t * D * 2 + Tile::v_place(t, d / 8) * 16 + d % 8 * 2);
+                        o[i][y] += see && (u & T::EXP) == T::EXP ? T::wide(u) : 0.f;
+                    }
+            }
+        }
+    };
+
+    auto clear = [&]() __attribute__((always_inline)) {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.f);
+    };
+    clear();
+    load(0, s_k0, s_v0);
+    for (int j = 0; j < blocks; j += 2) {
+        __syncthreads();  // this block has arrived, and everyone is done with the one before it
+        if (j + 1 < blocks) load(j + 1, s_k1, s_v1);
+        if (wlive && j * KB < wmost) block(std::false_type(), j, s_k0, s_v0);
+        if (j + 1 >= blocks) break;
+        __syncthreads();
+        if (j + 2 < blocks) load(j + 2, s_k0, s_v0);
+        if (wlive && (j + 1) * KB < wmost) block(std::false_type(), j + 1, s_k1, s_v1);
+    }
+    // A value that is not finite makes whole tiles so, whether or not their rows see it, through products with weights of 0: such
+    // tiles are worked out again.
+    float zero = 0.f * l;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) zero = __builtin_fmaf(0.f, o[i][y], zero);
+    if (__syncthreads_or(valid && zero != 0.f)) {
+        clear();
+        for (int j = 0; j < blocks; ++j) {
+            load(j, s_k0, s_v0);
+            __syncthreads();
+            if (wlive && j * KB < wmost) block(std::true_type(), j, s_k0, s_v0);
+            __syncthreads();
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+
+    const int64_t at = (int64_t)(begin + qi) * H * g + h * g + hg;
+    const float f = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const typename T::x2 p0 = T::narrow(o[i][4 * y] * f, o[i][4 * y + 1] * f), p1 = T::narrow(o[i][4 * y + 2] * f, o[i][4 * y + 3] * f);
+            *reinterpret_cast<uint2 *>(a.out + at * D + 32 * i + 8 * y + 4 * half) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+        }
+    if (half == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
