@@ -520,7 +520,7 @@ int etf_ivf_search(etf_ctx *ctx, const float *queries, int64_t Q, int k, int w, 
  *   lens    i32 [batch]                              tokens in each sequence's cache, the same for all its heads; counts as 0
  *                                                    below that and as 64 max_blocks + 63 above that
  *   evicted i32 [batch]                              blocks that etf_kv_evict has taken out of each sequence so far
- * A page belongs to one block of one head.  batch * heads * max_blocks < 2^31, and a call that needs a launch of 2^32
+ * A page belongs to one block of one head, or to several that hold the same (etf_kv_fork).  batch * heads * max_blocks < 2^31, and a call that needs a launch of 2^32
  * threads or more is refused; head_dim is 64, 96 or 128; all arrays 16-byte aligned.  lens is advanced by the caller (after
  * etf_kv_append, before etf_kv_attend with the new tokens' queries); it may be taken back to no less than what the full
  * blocks hold.  Where an append has completed one block, the last so far, it may also be taken back to what it was before
@@ -549,6 +549,12 @@ typedef struct etf_kv_cache {
  * rows that see it become not a number, no others do, and its block's scales and bounds leave it out. */
 int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v,
                   const int64_t *v_strides, int n, const int32_t *counts);
+
+/* The same for tokens that lie packed, one sequence's after the other's: sequence b's new tokens are [starts[b], starts[b + 1]) of
+ * k, v [tokens][heads][head_dim] (starts: i32 [batch + 1], device, ascending, within [0, tokens]; counts as 0 or as tokens outside of
+ * that, and a sequence whose end lies before its start has no new tokens).  strides[0..1]: elements from one token and head to the next. */
+int etf_kv_append_packed(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v, const int64_t *v_strides,
+                         int64_t tokens, const int32_t *starts);
 
 /* Attention over the cache: with s = scale * <q, k_t> over the tokens that a row sees, out = sum softmax(s)_t v_t (dense
  * [batch][n][heads_q][head_dim], the cache's type) and, where lse is not NULL, lse = log sum exp(s) (float [batch][n][heads_q]).
@@ -581,6 +587,38 @@ int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const 
  * 16384 blocks a row), or others that share nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1. */
 int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
                  int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
+
+/* Pages.  refs (i32 [pages], the caller's) holds how many entries of the table name each page; a page with none (0 or less) is free.  Pages
+ * of full blocks may be shared, by several sequences or by a table and what the caller keeps for later (one share each): the calls above
+ * read them, and write only to those of blocks that an append completes, which etf_kv_take gives pages of their own.  A table
+ * starts out with -1 throughout and refs with 0 (or with a page for every block, and refs with 1).
+ *
+ * etf_kv_take, ahead of etf_kv_append: every block that an append of counts tokens (i32 [batch]; NULL: all n) completes gets the lowest free
+ * page, in the order (sequence, head, block), unless it has one that no other entry names; one that it shares loses that share.
+ * Either all of them get one, or, where there are not enough free pages, none does: missing (i32 [1], device) says how many pages are
+ * lacking, 0 as a rule.  table_out, refs_out: the arrays they are read from, or others that share nothing with them. */
+int64_t etf_kv_take_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache, int n);
+int etf_kv_take(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs, int n, const int32_t *counts, int32_t *table_out, int32_t *refs_out,
+                int32_t *missing, void *ws, int64_t ws_bytes);
+
+/* Every sequence b becomes a copy of sequence source[b] as that was before the call (i32 [batch]; b itself: it stays; no sequence's
+ * number: it is emptied): the full blocks' pages are shared, the open block's tokens copied, lens and evicted taken over, entries
+ * behind the full blocks become -1; refs follow, also for the entries that were there before.  With keep (i32 [batch], or NULL) a copy
+ * of fewer than all tokens has the first keep[b] of them, in whole blocks: 64 * (keep[b] / 64), which may be its own first ones.
+ * The lens of a copy that is not a sequence itself may not be taken back below its open block (the tokens of the block before it
+ * are the source's).  Writes table, lens, evicted, tail_k, tail_v. */
+int64_t etf_kv_fork_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache);
+int etf_kv_fork(etf_ctx *ctx, const etf_kv_cache *cache, int32_t *refs, const int32_t *source, const int32_t *keep, void *ws, int64_t ws_bytes);
+
+/* One share less for each entry of list (i32 [n], device; etf_kv_evict's freed) that is a page of [0, pages), none below 0. */
+int etf_kv_free(etf_ctx *ctx, int32_t *refs, int pages, const int32_t *list, int64_t n);
+
+/* Brings the pages that are in use, U of them, to [0, U): the i-th free one below U takes what is in the used one that has i used ones behind
+ * it.  table_out, refs_out as above; used: i32 [1], device, = U.  Entries of the table that name free pages stay.  No other table may
+ * name pages of the pool. */
+int64_t etf_kv_compact_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache);
+int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *used, void *ws,
+                   int64_t ws_bytes);
 
 /* ---- attention over whole prompts ---------------------------------------- */
 

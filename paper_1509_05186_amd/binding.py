@@ -29,6 +29,8 @@ EXPORTS = [
     "etf_ivf_set_coarse", "etf_ivf_assign_workspace_bytes", "etf_ivf_assign_device", "etf_ivf_build", "etf_ivf_stats",
     "etf_ivf_device_bytes", "etf_ivf_upload", "etf_ivf_workspace_bytes", "etf_ivf_search",
     "etf_kv_append", "etf_kv_attend_workspace_bytes", "etf_kv_attend", "etf_kv_select_workspace_bytes", "etf_kv_select", "etf_kv_evict",
+    "etf_kv_append_packed", "etf_kv_take_workspace_bytes", "etf_kv_take", "etf_kv_fork_workspace_bytes", "etf_kv_fork", "etf_kv_free",
+    "etf_kv_compact_workspace_bytes", "etf_kv_compact",
     "etf_prompt_attend_workspace_bytes", "etf_prompt_attend",
 ]
 ETF_BUILD_NONE, ETF_BUILD_CHAIN, ETF_BUILD_GENERAL, ETF_BUILD_GENERAL_AFTER_CHAIN = 0, 1, 2, 3
@@ -194,6 +196,14 @@ def load_library():
         "etf_kv_select_workspace_bytes": (L, [P, P, I, I, I]),
         "etf_kv_select": (I, [P, P, P, P, I, I, P, I, I, I, P, P, L]),
         "etf_kv_evict": (I, [P, P, P, I, I, I, P, P, P, P, P]),
+        "etf_kv_append_packed": (I, [P, P, P, P, P, P, L, P]),
+        "etf_kv_take_workspace_bytes": (L, [P, P, I]),
+        "etf_kv_take": (I, [P, P, P, I, P, P, P, P, P, L]),
+        "etf_kv_fork_workspace_bytes": (L, [P, P]),
+        "etf_kv_fork": (I, [P, P, P, P, P, P, L]),
+        "etf_kv_free": (I, [P, P, I, P, L]),
+        "etf_kv_compact_workspace_bytes": (L, [P, P]),
+        "etf_kv_compact": (I, [P, P, P, P, P, P, P, L]),
         "etf_prompt_attend_workspace_bytes": (L, [P, I, L, I, I, I]),
         "etf_prompt_attend": (I, [P, I, I, P, P, P, P, P, P, L, I, I, P, I, ctypes.c_float, P, P, P, L]),
     }
@@ -845,6 +855,90 @@ class Context:
         c = (cache if to is None else to)._c
         self._ck(self._lib.etf_kv_evict(self._h, cache._ref, pm, budget, sink, recent, c.table, c.lens, c.evicted, po, pf))
         return mass_out, freed
+
+    def kv_append_packed(self, cache: KvCache, k, v, starts):
+        """kv_append for packed tokens: k, v [tokens][H][D], sequence b's new ones are [starts[b], starts[b + 1]), starts int32 [B + 1]; the
+        caller then advances cache.lens.  There is no gradient."""
+        import torch
+        self._kv_here(cache)
+        self._no_gradient(k, "k")
+        self._no_gradient(v, "v")
+        if k.dim() != 3 or k.dtype != cache.dtype or k.get_device() != cache._gpu or k.shape[0] < 1:
+            raise ValueError("k: expected a %s tensor [tokens][%d][%d] on %s" % (cache.dtype, cache.heads, cache.head_dim, cache.device))
+        pk, sk = self._packed(k, k.shape[0], cache.heads, cache.head_dim, k, "k")
+        pv, sv = self._packed(v, k.shape[0], cache.heads, cache.head_dim, k, "v")
+        ps = self._kv_dev(starts, (cache.batch + 1,), torch.int32, cache, "starts")
+        self._ck(self._lib.etf_kv_append_packed(self._h, cache._ref, pk, sk, pv, sv, k.shape[0], ps))
+
+    # ---- pages of the cache
+    def kv_take_workspace_bytes(self, cache: KvCache, n: int) -> int:
+        return self._ck(self._lib.etf_kv_take_workspace_bytes(self._h, cache._ref, n))
+
+    def kv_take(self, cache: KvCache, refs, n: int = 1, counts=None, table_out=None, refs_out=None, missing=None, ws=None):
+        """Gives the blocks that an append of counts tokens (None: n of each sequence) completes pages of their own from the free ones of refs
+        (int32 [pages]: how many entries name each).  All get one or none does: returns missing, int32 [1], the pages that are lacking.
+        table_out, refs_out: written instead of cache.table and refs."""
+        import torch
+        self._kv_here(cache)
+        pr = self._kv_dev(refs, (cache.pages,), torch.int32, cache, "refs")
+        pc = self._kv_dev(counts, (cache.batch,), torch.int32, cache, "counts")
+        pt = cache._c.table if table_out is None else self._kv_dev(table_out, (cache.batch, cache.heads, cache.max_blocks), torch.int32, cache, "table_out")
+        po = pr if refs_out is None else self._kv_dev(refs_out, (cache.pages,), torch.int32, cache, "refs_out")
+        if missing is None:
+            missing = self._kv_empty((1,), torch.int32, cache)
+        pm = self._kv_dev(missing, (1,), torch.int32, cache, "missing")
+        if ws is None:
+            ws = self._kv_scratch(cache, Context.kv_take_workspace_bytes, n)
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_kv_take(self._h, cache._ref, pr, n, pc, pt, po, pm, pw, nw))
+        return missing
+
+    def kv_fork_workspace_bytes(self, cache: KvCache) -> int:
+        return self._ck(self._lib.etf_kv_fork_workspace_bytes(self._h, cache._ref))
+
+    def kv_fork(self, cache: KvCache, refs, source, keep=None, ws=None):
+        """Sequence b becomes a copy of sequence source[b] (int32 [B]; b: it stays; -1: it is emptied), or of its first keep[b] tokens in whole
+        blocks: shared pages, an open block of its own.  Writes the cache's table, lens, evicted and open blocks, and refs."""
+        import torch
+        self._kv_here(cache)
+        pr = self._kv_dev(refs, (cache.pages,), torch.int32, cache, "refs")
+        ps = self._kv_dev(source, (cache.batch,), torch.int32, cache, "source")
+        pk = self._kv_dev(keep, (cache.batch,), torch.int32, cache, "keep")
+        if ws is None:
+            ws = self._kv_scratch(cache, Context.kv_fork_workspace_bytes)
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_kv_fork(self._h, cache._ref, pr, ps, pk, pw, nw))
+
+    def kv_free(self, refs, pages):
+        """One share less in refs (int32 [pages of the pool]) for each page of the int32 tensor pages (kv_evict's freed), entries of -1 aside."""
+        import torch
+        gpu = refs.get_device()
+        self._here(gpu, refs.device)
+        if refs.dim() != 1 or refs.shape[0] < 1:
+            raise ValueError("refs: expected a tensor [pages]")
+        pr = self._plain(refs, refs.shape, torch.int32, refs, "refs")
+        pl = self._plain(pages, pages.shape, torch.int32, refs, "pages")
+        self._ck(self._lib.etf_kv_free(self._h, pr, refs.shape[0], pl, pages.numel()))
+
+    def kv_compact_workspace_bytes(self, cache: KvCache) -> int:
+        return self._ck(self._lib.etf_kv_compact_workspace_bytes(self._h, cache._ref))
+
+    def kv_compact(self, cache: KvCache, refs, table_out=None, refs_out=None, used=None, ws=None):
+        """Brings the pages that refs says are in use to the front of the pool; returns used, int32 [1], how many they are.  table_out,
+        refs_out: written instead of cache.table and refs."""
+        import torch
+        self._kv_here(cache)
+        pr = self._kv_dev(refs, (cache.pages,), torch.int32, cache, "refs")
+        pt = cache._c.table if table_out is None else self._kv_dev(table_out, (cache.batch, cache.heads, cache.max_blocks), torch.int32, cache, "table_out")
+        po = pr if refs_out is None else self._kv_dev(refs_out, (cache.pages,), torch.int32, cache, "refs_out")
+        if used is None:
+            used = self._kv_empty((1,), torch.int32, cache)
+        pu = self._kv_dev(used, (1,), torch.int32, cache, "used")
+        if ws is None:
+            ws = self._kv_scratch(cache, Context.kv_compact_workspace_bytes)
+        pw, nw = self._ws(ws)
+        self._ck(self._lib.etf_kv_compact(self._h, cache._ref, pr, pt, po, pu, pw, nw))
+        return used
 
     # ---- attention over whole prompts
     def _here(self, gpu: int, device):

@@ -11,8 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIBDIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIBDIR, "libetf.so")
 
-SOURCES = ["etf_host.cpp", "etf_device.hip", "etf_build.hip", "etf_kv.hip", "etf_prompt.hip"]
-HEADERS = ["etf_internal.h", "etf_launch.h", "etf_kernels.hip.h", "etf_ctx_kernels.hip.h", "etf_ivf.hip.h", "etf_prune_kernels.hip.h", "etf_build_kernels.hip.h", "etf_kv_types.hip.h", "etf_kv_kernels.hip.h", "etf_prompt_kernels.hip.h"]
+SOURCES = ["etf_host.cpp", "etf_device.hip", "etf_build.hip", "etf_kv.hip", "etf_prompt.hip", "etf_pages.hip"]
+HEADERS = ["etf_internal.h", "etf_launch.h", "etf_kernels.hip.h", "etf_ctx_kernels.hip.h", "etf_ivf.hip.h", "etf_prune_kernels.hip.h", "etf_build_kernels.hip.h", "etf_kv_types.hip.h", "etf_kv_kernels.hip.h", "etf_prompt_kernels.hip.h", "etf_pages_kernels.hip.h"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

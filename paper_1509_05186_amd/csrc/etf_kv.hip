@@ -198,7 +198,45 @@ extern "C" int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     return with_shape(cache, [&](auto t, auto dim) {
         ProfScope prof(ctx, ETF_K_KV);
-        hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(dim)::value>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+        hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(dim)::value, false>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
+        LAUNCH_CHECK(ctx, "k_kv_append");
+        return (int)ETF_OK;
+    });
+}
+
+extern "C" int etf_kv_append_packed(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v, const int64_t *v_strides,
+                                    int64_t tokens, const int32_t *starts)
+{
+    int rc = check_cache(ctx, cache, true);
+    if (rc != ETF_OK) return rc;
+    if (tokens < 1 || tokens > INT32_MAX / 2) return fail(ctx, ETF_EINVAL, "need 1 <= tokens < 2^30 (tokens=%lld)", (long long)tokens);
+    if (!starts) return fail(ctx, ETF_EINVAL, "starts is null");
+    KvAppendArgs a{};
+    a.c = view_of(cache);
+    // strides of token and head, where rows of [1][tokens][heads] have that of a sequence in front
+    int64_t in[2][3], out[2][3];
+    const int64_t *given[2] = {k_strides, v_strides};
+    for (int i = 0; i < 2; ++i) {
+        if (given[i]) {
+            in[i][0] = 0;
+            in[i][1] = given[i][0];
+            in[i][2] = given[i][1];
+        }
+        if ((rc = check_rows(ctx, cache, i ? "v" : "k", i ? v : k, given[i] ? in[i] : nullptr, tokens, cache->heads, out[i])) != ETF_OK) return rc;
+    }
+    for (int i = 0; i < 2; ++i) {
+        a.ks[i] = out[0][i + 1];
+        a.vs[i] = out[1][i + 1];
+    }
+    a.k = (const uint16_t *)k;
+    a.v = (const uint16_t *)v;
+    a.seq = Packed{starts, (int)tokens, cache->batch};
+    const int64_t grid = (tokens / KB + cache->batch) * cache->heads;
+    if (too_many(grid)) return fail(ctx, ETF_EINVAL, "too many blocks for one call");
+    if ((rc = enter_device(ctx)) != ETF_OK) return rc;
+    return with_shape(cache, [&](auto t, auto dim) {
+        ProfScope prof(ctx, ETF_K_KV);
+        hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(dim)::value, true>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
         LAUNCH_CHECK(ctx, "k_kv_append");
         return (int)ETF_OK;
     });

@@ -52,6 +52,7 @@ struct KvAppendArgs {
     int64_t ks[3], vs[3];  // strides of sequence, token, head
     const int32_t *counts;
     int n, per;  // per: workgroups of a (sequence, head), the most blocks that n tokens can complete
+    Packed seq;  // packed tokens: their sequences, instead of counts and the strides of sequences
 };
 
 // Codes in the order of their values, two to a word: 16-bit numbers whose low byte is the code, its lower bits turned where it is
@@ -83,7 +84,7 @@ __device__ __forceinline__ int scale_exponent(float amax)
     return min(max(e - (m <= 0.875f ? 9 : 8), -126), 119);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool PACKED>
 __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
 {
     constexpr int PT = D / 8;                // 16-byte pieces of a token
@@ -97,13 +98,33 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     constexpr int BW = D / 4, BG = 256 / BW, BT = (KB + BG - 1) / BG;  // bounds: words of a row, groups of tokens, tokens of a group
     __shared__ __attribute__((aligned(8))) int16_t s_edge[2][BG][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t bh = blockIdx.x / a.per;
-    const int h = (int)(bh % a.c.heads), b = (int)(bh / a.c.heads), blk = blockIdx.x % a.per;
-    const int len = kv_len(a.c, b), count = min(kv_count(a.counts, b, a.n), a.c.blocks * KB + KB - 1 - len);  // as many as lens can count
+    int b, h, blk, given;
+    const uint16_t *nk = a.k, *nv = a.v;
+    if constexpr (PACKED) {
+        // a sequence of n tokens has floor(n / 64) + 1 numbers at least, as many workgroups as it can complete blocks
+        const int find = blockIdx.x / a.c.heads;
+        h = blockIdx.x % a.c.heads;
+        b = packed_of_tile<KB>(a.seq, 1, find);
+        const int start = packed_start(a.seq, b);
+        given = max(0, packed_start(a.seq, b + 1) - start);
+        blk = find - packed_base<KB>(a.seq, b, 1);
+        if (given == 0 || blk < 0) return;
+        nk += start * a.ks[0] + h * a.ks[1];
+        nv += start * a.vs[0] + h * a.vs[1];
+    } else {
+        const int64_t at = blockIdx.x / a.per;
+        h = (int)(at % a.c.heads);
+        b = (int)(at / a.c.heads);
+        blk = blockIdx.x % a.per;
+        given = kv_count(a.counts, b, a.n);
+        nk += b * a.ks[0] + h * a.ks[2];
+        nv += b * a.vs[0] + h * a.vs[2];
+    }
+    const int64_t bh = (int64_t)b * a.c.heads + h, tk = a.ks[PACKED ? 0 : 1], tv = a.vs[PACKED ? 0 : 1];
+    const int len = kv_len(a.c, b), count = min(given, a.c.blocks * KB + KB - 1 - len);  // as many as lens can count
     const int first = len / KB, begin = len % KB;
     const int full = (begin + count) / KB, left = (begin + count) % KB;
     if (blk > 0 && blk >= full) return;
-    const uint16_t *nk = a.k + b * a.ks[0] + h * a.ks[2], *nv = a.v + b * a.vs[0] + h * a.vs[2];
     if (tid < KB) s_bad[tid] = 0;
     __syncthreads();
     if (blk < full) {
@@ -115,8 +136,8 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
             const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
             const int at = blk * KB + t - begin;  // among the new tokens
             if (at >= 0) {
-                kw[i] = *reinterpret_cast<const uint4 *>(nk + at * a.ks[1] + d);
-                vw[i] = *reinterpret_cast<const uint4 *>(nv + at * a.vs[1] + d);
+                kw[i] = *reinterpret_cast<const uint4 *>(nk + at * tk + d);
+                vw[i] = *reinterpret_cast<const uint4 *>(nv + at * tv + d);
             } else {
                 kw[i] = *reinterpret_cast<const uint4 *>(a.c.tail_k + old + t * D + d);
                 uint16_t x[8];
@@ -221,7 +242,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
         for (int p = tid; p < np; p += 256) {
             const int t = from + p / PT, d = p % PT * 8;
             const int at = full * KB + t - begin;
-            uint4 kw = *reinterpret_cast<const uint4 *>(nk + at * a.ks[1] + d), vw = *reinterpret_cast<const uint4 *>(nv + at * a.vs[1] + d);
+            uint4 kw = *reinterpret_cast<const uint4 *>(nk + at * tk + d), vw = *reinterpret_cast<const uint4 *>(nv + at * tv + d);
             if (pass == 0) {
                 if (max(size8(kw), size8(vw)) >= T::EXP) s_bad[t] = 1;
                 continue;

@@ -1,5 +1,5 @@
 // What the kernels of the attention cache and of prompts' attention share: the 16-bit types with their matrix products, sizes of
-// numbers, and what softmax weights are taken against.  Included inside an anonymous namespace.
+// numbers, what softmax weights are taken against, and the numbering of packed sequences' tiles.  Included inside an anonymous namespace.
 #pragma once
 
 constexpr int KB = 64;  // tokens of a block
@@ -85,4 +85,32 @@ __device__ __forceinline__ typename T::x8 query8(typename T::x8 q)
     uint4 w = __builtin_bit_cast(uint4, q);
     if (size8(w) >= T::EXP) w.x = T::NOT | (uint32_t)T::NOT << 16;
     return __builtin_bit_cast(typename T::x8, w);
+}
+
+// Sequences that lie packed: sequence b has the tokens [starts[b], starts[b + 1]) of `tokens`.
+struct Packed {
+    const int32_t *starts;
+    int tokens, batch;
+};
+// first token of sequence b (b = batch: the end of the last), within the tokens that there are
+__device__ __forceinline__ int packed_start(const Packed &p, int b) { return min(max(p.starts[b], 0), p.tokens); }
+
+// All sequences share one numbering of tiles of ROWS rows, g rows to a token, that needs no counting: sequence b's tiles begin at number
+// floor(starts[b] g / ROWS) + b, since it has at most floor(n g / ROWS) + 1 of them.
+template <int ROWS>
+__device__ __forceinline__ int packed_base(const Packed &p, int b, int g) { return (int)((int64_t)packed_start(p, b) * g / ROWS) + b; }
+// The last sequence whose tiles begin at or before number `find`, or 0, by a search of 64 places at a time.  Every lane of the wave calls it.
+template <int ROWS>
+__device__ __forceinline__ int packed_of_tile(const Packed &p, int g, int find)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, many = p.batch;  // it is one of [lo, lo + many)
+    while (many > 1) {
+        const int step = (many + 63) / 64, i = lane * step;
+        const uint64_t before = __ballot(i < many && packed_base<ROWS>(p, min(lo + i, p.batch - 1), g) <= find);
+        const int last = before ? 63 - __builtin_clzll(before) : 0;
+        lo += last * step;
+        many = min(step, many - last * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
 }

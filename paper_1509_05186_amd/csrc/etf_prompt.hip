@@ -88,12 +88,10 @@ extern "C" int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const vo
     a.q = (const uint16_t *)q;
     a.k = (const uint16_t *)k;
     a.v = (const uint16_t *)v;
-    a.starts = starts;
+    a.seq = Packed{starts, (int)tokens, batch};
     a.out = (uint16_t *)out;
     a.lse = lse;
     a.scale2 = std::min(scale * 1.4426950408889634f, std::numeric_limits<float>::max());
-    a.tokens = (int)tokens;
-    a.batch = batch;
     a.heads = heads;
     a.g = heads_q / heads;
     if (ctx->device < 0) return fail(ctx, ETF_ENOGPU, "host-only context");

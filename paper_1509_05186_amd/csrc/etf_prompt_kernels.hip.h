@@ -6,35 +6,12 @@
 struct PromptArgs {
     const uint16_t *q, *k, *v;
     int64_t qs[2], ks[2], vs[2];  // strides of token, head
-    const int32_t *starts;
+    Packed seq;
     uint16_t *out;
     float *lse;
     float scale2;  // softmax scale times log2 e, finite
-    int tokens, batch, heads, g;
+    int heads, g;
 };
-
-// first token of sequence b (b = batch: the end of the last), within the tokens that there are
-__device__ __forceinline__ int prompt_start(const PromptArgs &a, int b) { return min(max(a.starts[b], 0), a.tokens); }
-
-// Sequences share one numbering of tiles that needs no counting: sequence b's tiles of ROWS rows begin at number floor(starts[b] g / ROWS) + b,
-// since it has at most floor(n g / ROWS) + 1 of them.  The last sequence that begins at or before `find`, by a search of
-// 64 places at a time.  Every lane of the wave calls it.
-template <int ROWS>
-__device__ __forceinline__ int prompt_of_tile(const PromptArgs &a, int find)
-{
-    const int lane = threadIdx.x & 63;
-    int lo = 0, many = a.batch;  // it is one of [lo, lo + many)
-    while (many > 1) {
-        const int step = (many + 63) / 64, i = lane * step;
-        const int b = lo + i;
-        const bool before = i < many && (int64_t)prompt_start(a, b) * a.g / ROWS + b <= find;
-        const uint64_t all = __ballot(before);
-        const int last = all ? 63 - __builtin_clzll(all) : 0;
-        lo += last * step;
-        many = min(step, many - last * step);
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
 
 // ------------------------------------------------------------------------------------------------
 // Attention of prompts in 16 bits.  Rows are pairs (token, query head of the group) of one sequence and key/value head, 128 to
@@ -75,9 +52,9 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
     const int H = a.heads, g = a.g;
     const int h = blockIdx.x % H, find = (int)(gridDim.x / H) - 1 - (int)(blockIdx.x / H);  // a prompt's last tiles, the longest ones, first
-    const int b = prompt_of_tile<ROWS>(a, find);
-    const int begin = __builtin_amdgcn_readfirstlane(prompt_start(a, b)), n = __builtin_amdgcn_readfirstlane(prompt_start(a, b + 1)) - begin;
-    const int tile = __builtin_amdgcn_readfirstlane(find - (int)((int64_t)begin * g / ROWS) - b);
+    const int b = packed_of_tile<ROWS>(a.seq, g, find);
+    const int begin = __builtin_amdgcn_readfirstlane(packed_start(a.seq, b)), n = __builtin_amdgcn_readfirstlane(packed_start(a.seq, b + 1)) - begin;
+    const int tile = find - __builtin_amdgcn_readfirstlane(packed_base<ROWS>(a.seq, b, g));
     if (n <= 0 || tile < 0 || (int64_t)tile * ROWS >= (int64_t)n * g) return;
     const int64_t rows = (int64_t)n * g, row0 = (int64_t)tile * ROWS, row = row0 + 32 * wave + x;
     const bool valid = row < rows;
