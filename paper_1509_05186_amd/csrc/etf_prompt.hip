@@ -14,6 +14,10 @@ namespace {
 
 #include "etf_prompt_kernels.hip.h"
 
+constexpr int64_t PROMPT_FEW = 768;    // (tile, head) units from which the card is full without ranges: it holds 512 workgroups at once
+constexpr int64_t PROMPT_LEAST = 8;    // blocks of a range, at least
+constexpr int64_t PROMPT_RANGES = 16;  // ranges of a tile, at most
+
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // strides of token and head of rows [tokens][heads][dim]
@@ -28,8 +32,12 @@ int check_packed(const etf_ctx *ctx, const char *what, const void *p, const int6
     return ETF_OK;
 }
 
+inline int64_t al256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+
+// How a call is cut up, and where its workspace's arrays lie.
 struct PromptPlan {
-    int64_t tiles = 0, grid = 0, total = 256;
+    int64_t tiles = 0, grid = 0, o_ml = 0, total = 256;  // tiles of one head that there can be
+    int ranges = 1, per = INT32_MAX;
 };
 
 int plan_prompt(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch, PromptPlan &p)
@@ -41,7 +49,24 @@ int plan_prompt(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, i
     if (heads_q % heads != 0) return fail(ctx, ETF_EINVAL, "heads_q (%d) must be a multiple of heads (%d)", heads_q, heads);
     if (tokens > INT32_MAX / heads_q || batch > (1 << 24)) return fail(ctx, ETF_EINVAL, "tokens * heads_q must stay below 2^31, batch up to 2^24");
     p.tiles = tokens * (heads_q / heads) / 128 + batch;
-    p.grid = p.tiles * heads;
+    // Few tiles do not fill the card, and the longest of them decides: their blocks are cut into ranges of `per`.  What that costs is the ranges' partial
+    // results, written and read again, about as much as 1 / 35 of a block's time for each of them, and the launch that joins them, four blocks':
+    // per blocks and units * longest / (2 per) partial results take the least together where both are sqrt(units * longest / 70).  The
+    // host knows the number of tokens, not the lengths: of several prompts the longest is taken to be twice the mean.
+    // One prompt, 128 dimensions: 4096 tokens, 2 heads 79 us uncut, 38 cut; 8000 tokens, 1 head 145 and 45; 8 heads, four query heads to each:
+    // 600 tokens 20 and 25, 1000 tokens 28 and 36, 2000 tokens 51 and 72, which are left uncut.
+    const int64_t units = p.tiles * heads, blocks = (tokens + KB - 1) / KB, longest = batch == 1 ? blocks : std::min(blocks, 2 * ((blocks + batch - 1) / batch));
+    const int64_t per = std::max<int64_t>(PROMPT_LEAST, (int64_t)std::sqrt(units * longest / 70.));
+    if (units < PROMPT_FEW && 2 * per + 4 <= longest * 17 / 20) {
+        p.per = (int)std::max(per, (blocks + PROMPT_RANGES - 1) / PROMPT_RANGES);
+        p.ranges = (int)((blocks + p.per - 1) / p.per);
+    }
+    if (p.ranges == 1) p.per = INT32_MAX;
+    p.grid = units * p.ranges;
+    if (p.ranges > 1) {
+        p.o_ml = al256(p.grid * 128 * head_dim * 4);
+        p.total = p.o_ml + al256(p.grid * 128 * 2 * 4);
+    }
     if (p.grid > (int64_t)UINT32_MAX / 256) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     return ETF_OK;
 }
@@ -52,6 +77,10 @@ int launch_prompt(etf_ctx *ctx, const PromptArgs &a, const PromptPlan &p)
     ProfScope prof(ctx, ETF_K_KV);
     hipLaunchKernelGGL((k_prompt<T, D>), dim3((unsigned)p.grid), dim3(256), 0, (hipStream_t)ctx->stream, a);
     LAUNCH_CHECK(ctx, "k_prompt");
+    if (p.ranges > 1) {
+        hipLaunchKernelGGL((k_prompt_join<T, D>), dim3((unsigned)(p.grid / p.ranges * 16)), dim3(256), 0, (hipStream_t)ctx->stream, a);
+        LAUNCH_CHECK(ctx, "k_prompt_join");
+    }
     return ETF_OK;
 }
 template <typename T>
@@ -94,6 +123,10 @@ extern "C" int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const vo
     a.scale2 = std::min(scale * 1.4426950408889634f, std::numeric_limits<float>::max());
     a.heads = heads;
     a.g = heads_q / heads;
+    a.ranges = p.ranges;
+    a.per = p.per;
+    a.part_o = (float *)ws;
+    a.part_ml = (float *)((char *)ws + p.o_ml);
     if (ctx->device < 0) return fail(ctx, ETF_ENOGPU, "host-only context");
     HIP_TRY(ctx, hipSetDevice(ctx->device));
     return dtype == ETF_KV_BF16 ? launch_prompt<TBf>(ctx, a, p, head_dim) : launch_prompt<THf>(ctx, a, p, head_dim);

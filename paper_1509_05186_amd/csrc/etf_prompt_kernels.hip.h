@@ -9,8 +9,10 @@ struct PromptArgs {
     Packed seq;
     uint16_t *out;
     float *lse;
+    float *part_o, *part_ml;  // partial results of ranges: [tile][head][range][128][D], [tile][head][range][128][2]
     float scale2;  // softmax scale times log2 e, finite
     int heads, g;
+    int ranges, per;  // most ranges of a tile's blocks, and blocks of one
 };
 
 // ------------------------------------------------------------------------------------------------
@@ -51,10 +53,11 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
     __shared__ __attribute__((aligned(1024))) uint8_t s_k0[KB * D * 2], s_v0[KB * D * 2], s_k1[KB * D * 2], s_v1[KB * D * 2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
     const int H = a.heads, g = a.g;
-    const int h = blockIdx.x % H, find = (int)(gridDim.x / H) - 1 - (int)(blockIdx.x / H);  // a prompt's last tiles, the longest ones, first
-    const int b = packed_of_tile<ROWS>(a.seq, g, find);
+    // a prompt's last tiles, the longest ones, first
+    const int h = blockIdx.x % H, range = blockIdx.x / H % a.ranges, number = gridDim.x / (H * a.ranges) - 1 - blockIdx.x / (H * a.ranges);
+    const int b = packed_of_tile<ROWS>(a.seq, g, number);
     const int begin = __builtin_amdgcn_readfirstlane(packed_start(a.seq, b)), n = __builtin_amdgcn_readfirstlane(packed_start(a.seq, b + 1)) - begin;
-    const int tile = find - __builtin_amdgcn_readfirstlane(packed_base<ROWS>(a.seq, b, g));
+    const int tile = number - __builtin_amdgcn_readfirstlane(packed_base<ROWS>(a.seq, b, g));
     if (n <= 0 || tile < 0 || (int64_t)tile * ROWS >= (int64_t)n * g) return;
     const int64_t rows = (int64_t)n * g, row0 = (int64_t)tile * ROWS, row = row0 + 32 * wave + x;
     const bool valid = row < rows;
@@ -62,7 +65,10 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
     const int sees = qi + 1;
     const int wleast = __builtin_amdgcn_readfirstlane(sees), wmost = __builtin_amdgcn_readfirstlane((int)(min(row0 + 32 * wave + 31, rows - 1) / g) + 1);
     const bool wlive = row0 + 32 * wave < rows;
-    const int most = (int)(min(row0 + ROWS - 1, rows - 1) / g) + 1, blocks = (most + KB - 1) / KB;
+    const int most = (int)(min(row0 + ROWS - 1, rows - 1) / g) + 1, all = (most + KB - 1) / KB;
+    const bool alone = all <= a.per;  // one range
+    const int from = alone ? 0 : range * a.per, blocks = min(from + a.per, all);
+    if (range > 0 && (alone || from >= all)) return;
 
     typename T::x8 q[ST];
     const uint16_t *qp = a.q + (begin + qi) * a.qs[0] + ((int64_t)h * g + hg) * a.qs[1];
@@ -131,7 +137,8 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);  // and what the lane 32 up or down has
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale;
         // z is s * scale less the reference with one rounding, as long as what rounding the largest z has left out matters no more than the others'
         // roundings; from there on, with one more, no z is above the largest: exponentials stay within the type.  Here and below a row goes by
         // its own numbers alone, so that its result does not depend on the rows beside it.
@@ -217,13 +224,17 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.f);
     };
+    // the wave's loads into LDS have arrived: the compiler does not wait for them at a barrier
+    auto arrived = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
     clear();
-    load(0, s_k0, s_v0);
-    for (int j = 0; j < blocks; j += 2) {
-        __syncthreads();  // this block has arrived, and everyone is done with the one before it
+    load(from, s_k0, s_v0);
+    for (int j = from; j < blocks; j += 2) {
+        arrived();
+        __syncthreads();  // this block is there, and everyone is done with the one before it
         if (j + 1 < blocks) load(j + 1, s_k1, s_v1);
         if (wlive && j * KB < wmost) block(std::false_type(), j, s_k0, s_v0);
         if (j + 1 >= blocks) break;
+        arrived();
         __syncthreads();
         if (j + 2 < blocks) load(j + 2, s_k0, s_v0);
         if (wlive && (j + 1) * KB < wmost) block(std::false_type(), j + 1, s_k1, s_v1);
@@ -237,8 +248,9 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
         for (int y = 0; y < 16; ++y) zero = __builtin_fmaf(0.f, o[i][y], zero);
     if (__syncthreads_or(valid && zero != 0.f)) {
         clear();
-        for (int j = 0; j < blocks; ++j) {
+        for (int j = from; j < blocks; ++j) {
             load(j, s_k0, s_v0);
+            arrived();
             __syncthreads();
             if (wlive && j * KB < wmost) block(std::true_type(), j, s_k0, s_v0);
             __syncthreads();
@@ -248,13 +260,55 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
     if (!valid) return;
 
     const int64_t at = (int64_t)(begin + qi) * H * g + h * g + hg;
-    const float f = 1.f / l;
+    if (alone) {
+        const float f = 1.f / l;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const typename T::x2 p0 = T::narrow(o[i][4 * y] * f, o[i][4 * y + 1] * f), p1 = T::narrow(o[i][4 * y + 2] * f, o[i][4 * y + 3] * f);
+                *reinterpret_cast<uint2 *>(a.out + at * D + 32 * i + 8 * y + 4 * half) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+            }
+        if (half == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        return;
+    }
+    const int64_t part = (((int64_t)number * H + h) * a.ranges + range) * ROWS + row - row0;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const typename T::x2 p0 = T::narrow(o[i][4 * y] * f, o[i][4 * y + 1] * f), p1 = T::narrow(o[i][4 * y + 2] * f, o[i][4 * y + 3] * f);
-            *reinterpret_cast<uint2 *>(a.out + at * D + 32 * i + 8 * y + 4 * half) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
-        }
-    if (half == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        for (int y = 0; y < 4; ++y)
+            *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * i + 8 * y + 4 * half) = (f32x4){o[i][4 * y], o[i][4 * y + 1], o[i][4 * y + 2], o[i][4 * y + 3]};
+    if (half == 0) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = make_float2(m, l);
+}
+
+// Joins the ranges of tiles that have several: 32 lanes to a row, eight rows to a workgroup.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a)
+{
+    constexpr int ROWS = 128, PARTS = ROWS / 8;
+    const int H = a.heads, g = a.g, lane = threadIdx.x & 31, y = blockIdx.x % PARTS * 8 + threadIdx.x / 32;
+    const int h = blockIdx.x / PARTS % H, number = blockIdx.x / (PARTS * H);
+    const int b = packed_of_tile<ROWS>(a.seq, g, number), tile = number - packed_base<ROWS>(a.seq, b, g);
+    const int begin = packed_start(a.seq, b), n = packed_start(a.seq, b + 1) - begin;
+    const int64_t rows = (int64_t)max(0, n) * g, row = (int64_t)tile * ROWS + y;
+    if (tile < 0 || row >= rows) return;
+    const int most = (int)(min((int64_t)(tile + 1) * ROWS - 1, rows - 1) / g) + 1, all = (most + KB - 1) / KB;
+    if (all <= a.per) return;
+    const int many = (all + a.per - 1) / a.per;
+    const int64_t first = ((int64_t)number * H + h) * a.ranges * ROWS + y;
+    float m = -INFINITY, l = 0.f;
+    for (int s = 0; s < many; ++s) m = fmaxf(m, a.part_ml[(first + s * ROWS) * 2]);
+    const float base = m == -INFINITY ? 0.f : m;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < many; ++s) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (first + s * ROWS) * 2);
+        const float weight = __builtin_amdgcn_exp2f(ml.x - base);
+        l += ml.y * weight;
+        if (lane < D / 4) o += *reinterpret_cast<const f32x4 *>(a.part_o + (first + s * ROWS) * D + 4 * lane) * weight;
+    }
+    const float f = 1.f / l;
+    const int64_t at = (int64_t)(begin + (int)(row / g)) * H * g + h * g + row % g;
+    const typename T::x2 p0 = T::narrow(o[0] * f, o[1] * f), p1 = T::narrow(o[2] * f, o[3] * f);
+    if (lane < D / 4) *reinterpret_cast<uint2 *>(a.out + at * D + 4 * lane) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+    if (lane == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }

@@ -95,6 +95,32 @@ def test_long_prompts_and_wide_groups(dtype, D, H, g, lens):
     against_oracle(q, k, v, starts_of(lens), "prompts %s D %d H %d g %d lens %s" % (dtype, D, H, g, lens))
 
 
+@pytest.mark.parametrize("dtype,D,H,g,lens", [(BF, 128, 1, 1, [2100]), (HF, 64, 1, 2, [1500]), (HF, 96, 2, 1, [1700, 1300]), (BF, 64, 1, 3, [64 * 24]), (BF, 128, 1, 1, [1, 64 * 30 + 1])])
+def test_ranges(dtype, D, H, g, lens):
+    """Few tiles of long prompts: their blocks are cut into ranges, and joined."""
+    gen = torch.Generator().manual_seed(6)
+    q, k, v = rows(gen, dtype, sum(lens), H * g, H, D)
+    assert etf.Context(device=None).prompt_attend_workspace_bytes(sum(lens), H * g, H, D, len(lens)) > 256
+    against_oracle(q, k, v, starts_of(lens), "ranges %s D %d H %d g %d lens %s" % (dtype, D, H, g, lens))
+
+
+def test_ranges_with_what_is_not_finite():
+    say("ranges, not finite")
+    gen = torch.Generator().manual_seed(7)
+    q, k, v = rows(gen, BF, 1800, 1, 1, 64)
+    clean, _ = run(q, k, v, [0, 1800])
+    for where in (3, 600, 1799):
+        for name, dims in (("v", [5]), ("k", list(range(64)))):
+            x = dict(k=k.clone(), v=v.clone())
+            x[name][where, 0, 5] = math.nan
+            out, _ = run(q, x["k"], x["v"], [0, 1800])
+            bad = torch.isnan(out.cpu())
+            want = torch.zeros_like(bad)
+            want[where:, :, dims] = True
+            assert torch.equal(bad, want), (name, where)
+            assert torch.equal(out.cpu()[~want], clean.cpu()[~want])
+
+
 @pytest.mark.parametrize("batch", [1, 63, 64, 65, 128, 129, 200, 4097])
 def test_many_sequences(batch):
     lens = [(7 * b) % 5 for b in range(batch)]
