@@ -135,12 +135,16 @@ extern "C" int etf_kv_take(etf_ctx *ctx, const etf_kv_cache *cache, const int32_
     a.refs_out = refs_out;
     a.missing = missing;
     a.n = n;
+    const int64_t grid = (a.slots.many + 255) / 256;
+    const int64_t copied = std::max<int64_t>(refs_out != refs ? cache->pages : 0, table_out != cache->table ? (int64_t)cache->batch * cache->heads * cache->max_blocks : 0);
+    const int64_t copies = std::min<int64_t>(512, (copied + 1023) / 1024);
+    if (too_many(grid)) return fail(ctx, ETF_EINVAL, "too many blocks for one call");
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
     ProfScope prof(ctx, ETF_K_KV);
     hipStream_t st = (hipStream_t)ctx->stream;
-    hipLaunchKernelGGL(k_kv_take_flags, dim3((unsigned)(a.free.chunks + a.slots.chunks)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_kv_take_flags, dim3((unsigned)(a.free.chunks + a.slots.chunks + copies)), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_take_flags");
-    hipLaunchKernelGGL(k_kv_take, dim3((unsigned)a.slots.chunks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_kv_take, dim3((unsigned)grid), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_take");
     return ETF_OK;
 }
@@ -176,7 +180,7 @@ extern "C" int etf_kv_fork(etf_ctx *ctx, const etf_kv_cache *cache, int32_t *ref
     ForkArgs a{};
     if ((rc = check_ws(ctx, ws, ws_bytes, plan_fork(cache, (char *)ws, a))) != ETF_OK) return rc;
     const int64_t grid = (int64_t)cache->batch * cache->heads;
-    if (too_many(grid)) return fail(ctx, ETF_EINVAL, "too many rows for one call");
+    if (too_many(3 * grid)) return fail(ctx, ETF_EINVAL, "too many rows for one call");
     a.c = view_of(cache);
     a.refs = refs;
     a.source = source;
@@ -187,7 +191,7 @@ extern "C" int etf_kv_fork(etf_ctx *ctx, const etf_kv_cache *cache, int32_t *ref
     hipStream_t st = (hipStream_t)ctx->stream;
     hipLaunchKernelGGL(k_kv_fork_plan, dim3((unsigned)grid), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_fork_plan");
-    hipLaunchKernelGGL(k_kv_fork, dim3((unsigned)grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_kv_fork, dim3((unsigned)(3 * grid)), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_fork");
     return ETF_OK;
 }
@@ -213,10 +217,9 @@ extern "C" int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int
     a.table_out = table_out;
     a.refs_out = refs_out;
     a.used = used;
-    a.row = cache->head_dim;
     // no more than half of the pages can move
     const int64_t entries = (int64_t)cache->batch * cache->heads * cache->max_blocks;
-    a.movers = (int)std::min<int64_t>(2048, cache->pages / 2 / 16 + 1);
+    a.movers = (int)std::min<int64_t>(2048, cache->pages / 2 + 1);
     a.tables = (int)std::min<int64_t>(1024, (entries + 255) / 256);
     const int rest = (int)std::min<int64_t>(256, ((int64_t)cache->pages + 255) / 256);
     if ((rc = enter_device(ctx)) != ETF_OK) return rc;
@@ -224,7 +227,10 @@ extern "C" int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int
     hipStream_t st = (hipStream_t)ctx->stream;
     hipLaunchKernelGGL(k_kv_used_flags, dim3((unsigned)a.taken.chunks), dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_used_flags");
-    hipLaunchKernelGGL(k_kv_compact, dim3((unsigned)(a.movers + a.tables + rest)), dim3(256), 0, st, a);
+    const dim3 grid((unsigned)(a.movers + a.tables + rest));
+    if (cache->head_dim == 64) hipLaunchKernelGGL(k_kv_compact<64>, grid, dim3(256), 0, st, a);
+    else if (cache->head_dim == 96) hipLaunchKernelGGL(k_kv_compact<96>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(k_kv_compact<128>, grid, dim3(256), 0, st, a);
     LAUNCH_CHECK(ctx, "k_kv_compact");
     return ETF_OK;
 }

@@ -197,9 +197,10 @@ __device__ __forceinline__ int slot_column(const TakeArgs &a, int64_t slot, int6
 __global__ __launch_bounds__(256) void k_kv_take_flags(TakeArgs a)
 {
     __shared__ int s_sum[4];
+    const int chunks = a.free.chunks + a.slots.chunks;
     if ((int)blockIdx.x < a.free.chunks) {
         put_flags(a.free, blockIdx.x, s_sum, [&](int64_t i) { return a.refs[i] <= 0; });
-    } else {
+    } else if ((int)blockIdx.x < chunks) {
         put_flags(a.slots, blockIdx.x - a.free.chunks, s_sum, [&](int64_t i) {
             int64_t bh;
             const int j = slot_column(a, i, bh);
@@ -208,55 +209,49 @@ __global__ __launch_bounds__(256) void k_kv_take_flags(TakeArgs a)
             if (shares != 1) a.shared[i] = shares > 1 ? p : -1;
             return shares != 1;
         });
+    } else {  // outputs that lie elsewhere
+        const int64_t at = (int64_t)(blockIdx.x - chunks) * 256 + threadIdx.x, step = (int64_t)(gridDim.x - chunks) * 256;
+        if (a.refs_out != a.refs)
+            for (int64_t i = at; i < a.c.pages; i += step) a.refs_out[i] = a.refs[i];
+        if (a.table_out != a.c.table)
+            for (int64_t i = at; i < (int64_t)a.c.batch * a.c.heads * a.c.blocks; i += step) a.table_out[i] = a.c.table[i];
     }
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
-    if (a.refs_out != a.refs)
-        for (int64_t i = at; i < a.c.pages; i += step) a.refs_out[i] = a.refs[i];
-    if (a.table_out != a.c.table)
-        for (int64_t i = at; i < (int64_t)a.c.batch * a.c.heads * a.c.blocks; i += step) a.table_out[i] = a.c.table[i];
 }
 
+// 256 slots to a workgroup
 __global__ __launch_bounds__(256) void k_kv_take(TakeArgs a)
 {
     __shared__ int s_upto[PAGE_CHUNKS + 1], s_sum[4];
-    int need = 0, mine = 0, first = 0, there = 0;  // slots that want a page: of all, of this chunk, of the chunks before it; free pages
+    const int parts = a.slots.size / 256, chunk = blockIdx.x / parts;
+    const int64_t w0 = (int64_t)chunk * a.slots.size / 64, slot = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int need = 0, first = 0, there = 0;  // slots that want a page: of all, before this workgroup's; free pages
     for (int i = threadIdx.x; i < a.slots.chunks; i += 256) {
         const int x = a.slots.counts[i];
         need += x;
-        first += i < (int)blockIdx.x ? x : 0;
-        mine += i == (int)blockIdx.x ? x : 0;
+        first += i < chunk ? x : 0;
     }
-    need = group_sum(need, s_sum);
-    first = group_sum(first, s_sum);
-    mine = group_sum(mine, s_sum);
+    for (int64_t w = w0 + threadIdx.x; w < (int64_t)blockIdx.x * 4; w += 256) first += __popcll(a.slots.words[w]);
     for (int i = threadIdx.x; i < a.free.chunks; i += 256) there += a.free.counts[i];
+    need = group_sum(need, s_sum);
     there = group_sum(there, s_sum);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.missing = max(0, need - there);
-    if (need > there || mine == 0) return;
+    if (need == 0 || need > there) return;
+    first = group_sum(first, s_sum);
     const Ranks free = ranks_of(a.free, s_upto, s_sum);
-    const int64_t from = (int64_t)blockIdx.x * a.slots.size;
-    for (int i0 = 0; i0 < a.slots.size; i0 += 256) {
-        const int64_t slot = from + i0 + threadIdx.x;
-        const uint64_t word = a.slots.words[slot / 64];
-        const bool want = word >> (slot & 63) & 1;
-        // slots of this round before the wave's
-        const int wave = threadIdx.x >> 6;
-        int before = __popcll(word & ((1ull << (slot & 63)) - 1)), all = 0;
-        for (int w = 0; w < 4; ++w) {
-            const int n = __popcll(a.slots.words[(from + i0) / 64 + w]);
-            all += n;
-            before += w < wave ? n : 0;
-        }
-        if (want) {
-            int64_t bh;
-            const int j = slot_column(a, slot, bh);
-            const int page = (int)free.find<true>(first + before), shared = a.shared[slot];
-            a.table_out[bh * a.c.blocks + j] = page;
-            a.refs_out[page] = 1;
-            if (shared >= 0) atomicSub(a.refs_out + shared, 1);
-        }
-        first += all;
+    const int wave = threadIdx.x >> 6;
+    uint64_t word = 0;
+    for (int w = 0; w < 4; ++w) {
+        const uint64_t x = a.slots.words[(int64_t)blockIdx.x * 4 + w];
+        first += w < wave ? __popcll(x) : 0;
+        word = w == wave ? x : word;
     }
+    if (!(word >> (slot & 63) & 1)) return;
+    int64_t bh;
+    const int j = slot_column(a, slot, bh), shared = a.shared[slot];
+    const int page = (int)free.find<true>(first + __popcll(word & ((1ull << (slot & 63)) - 1)));
+    a.table_out[bh * a.c.blocks + j] = page;
+    a.refs_out[page] = 1;
+    if (shared >= 0) atomicSub(a.refs_out + shared, 1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -269,7 +264,6 @@ struct CompactArgs {
     const int32_t *refs;
     int32_t *table_out, *refs_out, *used;
     Flags taken;
-    int row;    // head_dim
     int movers, tables;  // workgroups that move pages, that rewrite the table; the others rewrite refs
 };
 
@@ -279,45 +273,50 @@ __global__ __launch_bounds__(256) void k_kv_used_flags(CompactArgs a)
     put_flags(a.taken, blockIdx.x, s_sum, [&](int64_t i) { return a.refs[i] > 0; });
 }
 
+// 64 x D bytes
+template <int D>
+__device__ __forceinline__ void move_page(uint8_t *of, int64_t to, int64_t from, int tid)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int PIECES = PAGE_KB * D / 16, EACH = (PIECES + 255) / 256;
+    u32x4 w[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (PIECES % 256 == 0 || tid + 256 * i < PIECES) w[i] = reinterpret_cast<const u32x4 *>(of + from * (PAGE_KB * D))[tid + 256 * i];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (PIECES % 256 == 0 || tid + 256 * i < PIECES) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4 *>(of + to * (PAGE_KB * D)) + tid + 256 * i);
+}
+
+template <int D>
 __global__ __launch_bounds__(256) void k_kv_compact(CompactArgs a)
 {
-    constexpr int PAIRS = 16;  // pages that a workgroup moves at a time
+    constexpr int PAIRS = 16;  // pages that a workgroup moves, at most, before it looks for others
     __shared__ int s_upto[PAGE_CHUNKS + 1], s_sum[4], s_pair[PAIRS][2];
     const Ranks taken = ranks_of(a.taken, s_upto, s_sum);
     const int used = taken.all(), moving = used - taken.before(used), tid = threadIdx.x;
     if ((int)blockIdx.x < a.movers) {
         if (blockIdx.x == 0 && tid == 0) *a.used = used;
-        const int bytes = PAGE_KB * a.row;  // of a page's keys, and of its values
-        for (int64_t i0 = (int64_t)blockIdx.x * PAIRS; i0 < moving; i0 += (int64_t)a.movers * PAIRS) {
+        const int each = min(PAIRS, (moving + a.movers - 1) / a.movers);
+        for (int64_t i0 = (int64_t)blockIdx.x * each; i0 < moving; i0 += (int64_t)a.movers * each) {
+            const int many = (int)min<int64_t>(each, moving - i0);
             __syncthreads();
-            if (tid < PAIRS * 2 && i0 + tid / 2 < moving) s_pair[tid / 2][tid % 2] = tid % 2 ? (int)taken.find<true>(used - 1 - (int)(i0 + tid / 2)) : (int)taken.find<false>((int)(i0 + tid / 2));
+            if (tid < many) s_pair[tid][0] = (int)taken.find<false>((int)(i0 + tid));
+            if (tid >= 64 && tid - 64 < many) s_pair[tid - 64][1] = (int)taken.find<true>(used - 1 - (int)(i0 + tid - 64));
             __syncthreads();
-            const int many = (int)min<int64_t>(PAIRS, moving - i0);
             if (tid < many) {
                 const int64_t to = s_pair[tid][0], from = s_pair[tid][1];
-                const float s0 = a.c.scales[from * 2], s1 = a.c.scales[from * 2 + 1];
+                const float2 scales = reinterpret_cast<const float2 *>(a.c.scales)[from];
                 const int shares = a.refs[from];
-                a.c.scales[to * 2] = s0;
-                a.c.scales[to * 2 + 1] = s1;
+                reinterpret_cast<float2 *>(a.c.scales)[to] = scales;
                 a.refs_out[to] = shares;
                 a.refs_out[from] = 0;
             }
             for (int y = 0; y < many; ++y) {
                 const int64_t to = s_pair[y][0], from = s_pair[y][1];
-                // a page's keys, then its values, up to four pieces of 16 bytes to a thread, all asked for before the first is written
-                uint4 w[4], edge = make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = (tid + 256 * i) * 16;
-                    if (at < 2 * bytes) w[i] = *reinterpret_cast<const uint4 *>(at < bytes ? a.c.k + from * bytes + at : a.c.v + from * bytes + at - bytes);
-                }
-                if (tid < 2 * a.row / 16) edge = reinterpret_cast<const uint4 *>(a.c.bounds + from * 2 * a.row)[tid];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = (tid + 256 * i) * 16;
-                    if (at < 2 * bytes) *reinterpret_cast<uint4 *>(at < bytes ? a.c.k + to * bytes + at : a.c.v + to * bytes + at - bytes) = w[i];
-                }
-                if (tid < 2 * a.row / 16) reinterpret_cast<uint4 *>(a.c.bounds + to * 2 * a.row)[tid] = edge;
+                move_page<D>(a.c.k, to, from, tid);
+                move_page<D>(a.c.v, to, from, tid);
+                if (tid < 2 * D / 16) reinterpret_cast<uint4 *>(a.c.bounds + to * 2 * D)[tid] = reinterpret_cast<const uint4 *>(a.c.bounds + from * 2 * D)[tid];
             }
         }
         return;
@@ -419,33 +418,39 @@ __global__ __launch_bounds__(256) void k_kv_fork_plan(ForkArgs a)
     for (int i = threadIdx.x; i < D * 8; i += 256) reinterpret_cast<uint4 *>(a.save_v + save)[i] = reinterpret_cast<const uint4 *>(a.c.tail_v + tail)[i];
 }
 
+// Three workgroups to a (sequence, head): its row of the table, its open block's keys, its values
 __global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a)
 {
-    const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.c.heads), h = (int)(bh % a.c.heads), D = a.row;
+    const int64_t bh = blockIdx.x / 3;
+    const int part = blockIdx.x % 3, b = (int)(bh / a.c.heads), h = (int)(bh % a.c.heads), D = a.row;
     const int4 plan = a.plan[b];
     const int what = plan.x, s = plan.y, tokens = plan.z, evicted = plan.w, full = tokens / PAGE_KB, left = tokens % PAGE_KB;
     if (what == FORK_STAYS) return;
     const int64_t from = (int64_t)s * a.c.heads + h;
-    const int32_t *row = what == FORK_COPY ? a.c.table + from * a.c.blocks : a.rows + bh * a.c.blocks;
-    int32_t *mine = a.c.table + bh * a.c.blocks;
-    for (int j = threadIdx.x; j < a.c.blocks; j += 256) {
-        const int old = mine[j];
-        if (what == FORK_CUT && j < full) continue;
-        const int now = j < full && what != FORK_EMPTY ? row[j] : -1;
-        if (now == old && what != FORK_CUT) continue;
-        if (page_valid(a.c, old)) atomicSub(a.refs + old, 1);
-        if (page_valid(a.c, now)) atomicAdd(a.refs + now, 1);
-        mine[j] = now;
-    }
-    if (h == 0 && threadIdx.x == 0) {
-        a.c.lens[b] = tokens;
-        a.c.evicted[b] = evicted;
+    if (part == 0) {
+        const int32_t *row = what == FORK_COPY ? a.c.table + from * a.c.blocks : a.rows + bh * a.c.blocks;
+        int32_t *mine = a.c.table + bh * a.c.blocks;
+        for (int j = threadIdx.x; j < a.c.blocks; j += 256) {
+            if (what == FORK_CUT && j < full) continue;
+            const int old = mine[j], now = j < full && what != FORK_EMPTY ? row[j] : -1;
+            if (now == old) continue;
+            if (page_valid(a.c, old)) atomicSub(a.refs + old, 1);
+            if (page_valid(a.c, now)) atomicAdd(a.refs + now, 1);
+            mine[j] = now;
+        }
+        if (h == 0 && threadIdx.x == 0) {
+            a.c.lens[b] = tokens;
+            a.c.evicted[b] = evicted;
+        }
+        return;
     }
     if (left == 0 || what == FORK_CUT) return;
     const int half = (full + evicted) & 1;
     const int64_t tail = (bh * 2 + half) * PAGE_KB * D, other = what == FORK_COPY ? (from * 2 + half) * PAGE_KB * D : bh * PAGE_KB * D;
-    const uint16_t *fk = (what == FORK_COPY ? a.c.tail_k : a.save_k) + other, *fv = (what == FORK_COPY ? a.c.tail_v : a.save_v) + other;
-    for (int i = threadIdx.x; i < left * D / 8; i += 256) reinterpret_cast<uint4 *>(a.c.tail_k + tail)[i] = reinterpret_cast<const uint4 *>(fk)[i];
-    copy_open_values(fv, a.c.tail_v + tail, D, left);
+    if (part == 2) {
+        copy_open_values((what == FORK_COPY ? a.c.tail_v : a.save_v) + other, a.c.tail_v + tail, D, left);
+        return;
+    }
+    const uint16_t *keys = (what == FORK_COPY ? a.c.tail_k : a.save_k) + other;
+    for (int i = threadIdx.x; i < left * D / 8; i += 256) reinterpret_cast<uint4 *>(a.c.tail_k + tail)[i] = reinterpret_cast<const uint4 *>(keys)[i];
 }
