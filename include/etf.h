@@ -634,7 +634,7 @@ int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs,
  *           whose end lies before its start, has no rows
  *   out     dense [tokens][heads_q][head_dim], the rows' type; lse: NULL or float [tokens][heads_q].  Rows of tokens that
  *           are no sequence's are left as they were
- *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes
+ *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes; any where that is 0
  * A row whose query, or of which a key that it sees, makes a logit +inf or not a number becomes not a number; a value that is not finite
  * makes its dimension so, in the rows that see it and in no other. */
 int64_t etf_prompt_attend_workspace_bytes(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch);

@@ -861,16 +861,25 @@ class Context:
         caller then advances cache.lens.  There is no gradient."""
         import torch
         self._kv_here(cache)
-        self._no_gradient(k, "k")
-        self._no_gradient(v, "v")
-        if k.dim() != 3 or k.dtype != cache.dtype or k.get_device() != cache._gpu or k.shape[0] < 1:
-            raise ValueError("k: expected a %s tensor [tokens][%d][%d] on %s" % (cache.dtype, cache.heads, cache.head_dim, cache.device))
-        pk, sk = self._packed(k, k.shape[0], cache.heads, cache.head_dim, k, "k")
-        pv, sv = self._packed(v, k.shape[0], cache.heads, cache.head_dim, k, "v")
+        if k.requires_grad or v.requires_grad:
+            self._no_gradient(k, "k")
+            self._no_gradient(v, "v")
+        like, tokens = (cache.dtype, cache._gpu), k.shape[0]
+        pk, sk = self._packed(k, (tokens, cache.heads, cache.head_dim), like, "k")
+        pv, sv = self._packed(v, (tokens, cache.heads, cache.head_dim), like, "v")
         ps = self._kv_dev(starts, (cache.batch + 1,), torch.int32, cache, "starts")
-        self._ck(self._lib.etf_kv_append_packed(self._h, cache._ref, pk, sk, pv, sv, k.shape[0], ps))
+        rc = self._lib.etf_kv_append_packed(self._h, cache._ref, pk, sk, pv, sv, tokens, ps)
+        if rc < 0:
+            self._ck(rc)
 
     # ---- pages of the cache
+    def _kv_int(self, cache: KvCache):
+        """An int32 [1] of the context's stream."""
+        if _current_stream(cache._gpu) == (self._stream or 0):
+            return cache._t["lens"].new_empty(1)
+        import torch
+        return self._kv_empty((1,), torch.int32, cache)
+
     def kv_take_workspace_bytes(self, cache: KvCache, n: int) -> int:
         return self._ck(self._lib.etf_kv_take_workspace_bytes(self._h, cache._ref, n))
 
@@ -885,12 +894,16 @@ class Context:
         pt = cache._c.table if table_out is None else self._kv_dev(table_out, (cache.batch, cache.heads, cache.max_blocks), torch.int32, cache, "table_out")
         po = pr if refs_out is None else self._kv_dev(refs_out, (cache.pages,), torch.int32, cache, "refs_out")
         if missing is None:
-            missing = self._kv_empty((1,), torch.int32, cache)
-        pm = self._kv_dev(missing, (1,), torch.int32, cache, "missing")
+            missing = self._kv_int(cache)
+            pm = missing.data_ptr()
+        else:
+            pm = self._kv_dev(missing, (1,), torch.int32, cache, "missing")
         if ws is None:
             ws = self._kv_scratch(cache, Context.kv_take_workspace_bytes, n)
         pw, nw = self._ws(ws)
-        self._ck(self._lib.etf_kv_take(self._h, cache._ref, pr, n, pc, pt, po, pm, pw, nw))
+        rc = self._lib.etf_kv_take(self._h, cache._ref, pr, n, pc, pt, po, pm, pw, nw)
+        if rc < 0:
+            self._ck(rc)
         return missing
 
     def kv_fork_workspace_bytes(self, cache: KvCache) -> int:
@@ -913,12 +926,13 @@ class Context:
         """One share less in refs (int32 [pages of the pool]) for each page of the int32 tensor pages (kv_evict's freed), entries of -1 aside."""
         import torch
         gpu = refs.get_device()
-        self._here(gpu, refs.device)
-        if refs.dim() != 1 or refs.shape[0] < 1:
-            raise ValueError("refs: expected a tensor [pages]")
-        pr = self._plain(refs, refs.shape, torch.int32, refs, "refs")
-        pl = self._plain(pages, pages.shape, torch.int32, refs, "pages")
-        self._ck(self._lib.etf_kv_free(self._h, pr, refs.shape[0], pl, pages.numel()))
+        if gpu != self._device and self._device is not None:
+            raise ValueError("refs is on %s, the context on GPU %d" % (refs.device, self._device))
+        if refs.dim() != 1 or refs.dtype != torch.int32 or not refs.is_contiguous():
+            raise ValueError("refs: expected a contiguous int32 tensor [pages]")
+        if pages.dtype != torch.int32 or not pages.is_contiguous() or pages.get_device() != gpu:
+            raise ValueError("pages: expected a contiguous int32 tensor on %s" % refs.device)
+        self._ck(self._lib.etf_kv_free(self._h, refs.data_ptr(), refs.numel(), pages.data_ptr(), pages.numel()))
 
     def kv_compact_workspace_bytes(self, cache: KvCache) -> int:
         return self._ck(self._lib.etf_kv_compact_workspace_bytes(self._h, cache._ref))
@@ -932,8 +946,10 @@ class Context:
         pt = cache._c.table if table_out is None else self._kv_dev(table_out, (cache.batch, cache.heads, cache.max_blocks), torch.int32, cache, "table_out")
         po = pr if refs_out is None else self._kv_dev(refs_out, (cache.pages,), torch.int32, cache, "refs_out")
         if used is None:
-            used = self._kv_empty((1,), torch.int32, cache)
-        pu = self._kv_dev(used, (1,), torch.int32, cache, "used")
+            used = self._kv_int(cache)
+            pu = used.data_ptr()
+        else:
+            pu = self._kv_dev(used, (1,), torch.int32, cache, "used")
         if ws is None:
             ws = self._kv_scratch(cache, Context.kv_compact_workspace_bytes)
         pw, nw = self._ws(ws)
@@ -941,42 +957,21 @@ class Context:
         return used
 
     # ---- attention over whole prompts
-    def _here(self, gpu: int, device):
-        if gpu != self._device and self._device is not None:
-            raise ValueError("the tensors are on %s, the context on GPU %d" % (device, self._device))
-
-    def _empty(self, gpu: int, like, shape, dtype):
-        """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
-        import torch
-        mine = self._stream or 0
-        if gpu < 0 or _current_stream(gpu) == mine:
-            return torch.empty(shape, dtype=dtype, device=like.device)
-        # torch takes a stream of its pool for a pointer of zero
-        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=like.device) if mine else torch.cuda.default_stream(like.device)):
-            return torch.empty(shape, dtype=dtype, device=like.device)
-
     @staticmethod
-    def _packed(t, tokens, heads, dim, like, what: str):
-        """(pointer, strides) of rows [tokens][heads][dim]; dense ones need no strides."""
-        if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or t.shape[2] != dim or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads):
-            raise ValueError("%s: expected a %s tensor [%d][%s][%d] on %s" % (what, like.dtype, tokens, "heads" if heads is None else heads, dim, like.device))
+    def _packed(t, shape, like, what: str):
+        """(pointer, strides) of rows [tokens][heads][dim] of the type and on the GPU of `like`; dense ones need no strides."""
+        if t.shape != shape or (t.dtype, t.get_device()) != like:
+            raise ValueError("%s: expected a %s tensor %s on %s" % (what, like[0], list(shape), "cuda:%d" % like[1] if like[1] >= 0 else "the CPU"))
         if t.is_contiguous():
             return t.data_ptr(), None
         s = t.stride()
         if s[2] != 1:
             raise ValueError("%s: a row's elements must be contiguous" % what)
         # of a dimension of one torch allows any stride, which nothing uses
-        return t.data_ptr(), (ctypes.c_int64 * 2)(*(s[i] if t.shape[i] > 1 else 0 for i in range(2)))
-
-    @staticmethod
-    def _plain(t, shape, dtype, like, what: str):
-        if t is None:
-            return None
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
-            raise ValueError("%s: expected a contiguous %s tensor %s on %s" % (what, dtype, list(shape), like.device))
-        return t.data_ptr()
+        return t.data_ptr(), (ctypes.c_int64 * 2)(*(s[i] if shape[i] > 1 else 0 for i in range(2)))
 
     def prompt_attend_workspace_bytes(self, tokens: int, heads_q: int, heads: int, head_dim: int, batch: int) -> int:
+        """Bytes of the workspace, 0 where none is needed."""
         return self._ck(self._lib.etf_prompt_attend_workspace_bytes(self._h, head_dim, tokens, heads_q, heads, batch))
 
     def prompt_attend(self, q, k, v, starts, scale: Optional[float] = None, out=None, lse=None, ws=None):
@@ -985,29 +980,51 @@ class Context:
         Rows of tokens that are no sequence's are left as they were.  There is no gradient: tensors that require one are refused
         where torch would record it."""
         import torch
-        for t, what in ((q, "q"), (k, "k"), (v, "v")):
-            self._no_gradient(t, what)
-        if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16):
+        if q.requires_grad or k.requires_grad or v.requires_grad:
+            for t, what in ((q, "q"), (k, "k"), (v, "v")):
+                self._no_gradient(t, what)
+        dtype, gpu, shape, of_k = q.dtype, q.get_device(), q.shape, k.shape
+        if len(shape) != 3 or len(of_k) != 3 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
             raise ValueError("expected q [tokens][heads_q][D] and k [tokens][heads][D], bfloat16 or float16")
-        (tokens, heads_q, D), heads, gpu = q.shape, k.shape[1], q.get_device()
-        self._here(gpu, q.device)
-        pq, sq = self._packed(q, tokens, None, D, q, "q")
-        pk, sk = self._packed(k, tokens, heads, D, q, "k")
-        pv, sv = self._packed(v, tokens, heads, D, q, "v")
-        if starts.dim() != 1 or starts.shape[0] < 2:
-            raise ValueError("starts: expected a tensor [B + 1], B at least 1")
-        batch = starts.shape[0] - 1
-        ps = self._plain(starts, (batch + 1,), torch.int32, q, "starts")
+        if gpu != self._device and self._device is not None:
+            raise ValueError("q is on %s, the context on GPU %d" % (q.device, self._device))
+        (tokens, heads_q, D), heads, like = shape, of_k[1], (dtype, gpu)
+        pq, sq = self._packed(q, shape, like, "q")
+        pk, sk = self._packed(k, (tokens, heads, D), like, "k")
+        pv, sv = self._packed(v, (tokens, heads, D), like, "v")
+        batch = starts.numel() - 1
+        if batch < 1 or starts.dim() != 1 or starts.dtype != torch.int32 or not starts.is_contiguous() or starts.get_device() != gpu:
+            raise ValueError("starts: expected a contiguous int32 tensor [B + 1] on %s, B at least 1" % q.device)
+        here = gpu < 0 or _current_stream(gpu) == (self._stream or 0)
         if out is None:
-            out = self._empty(gpu, q, q.shape, q.dtype)
-        po = self._plain(out, q.shape, q.dtype, q, "out")
-        pe = self._plain(lse, (tokens, heads_q), torch.float32, q, "lse")
-        if ws is None:
-            ws = self._empty(gpu, q, (self.prompt_attend_workspace_bytes(tokens, heads_q, heads, D, batch) + 256,), torch.uint8)
-        pw, nw = self._ws(ws)
-        self._ck(self._lib.etf_prompt_attend(self._h, ETF_KV_BF16 if q.dtype == torch.bfloat16 else ETF_KV_FP16, D, pq, sq, pk, sk, pv, sv, tokens, heads_q, heads,
-                                             ps, batch, D ** -0.5 if scale is None else scale, po, pe, pw, nw))
+            out = torch.empty_like(q, memory_format=torch.contiguous_format) if here else self._empty(q, shape, dtype)
+        elif out.shape != shape or out.dtype != dtype or not out.is_contiguous() or out.get_device() != gpu:
+            raise ValueError("out: expected a contiguous %s tensor %s on %s" % (dtype, list(shape), q.device))
+        if lse is not None and (lse.shape != (tokens, heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != gpu):
+            raise ValueError("lse: expected a contiguous float32 tensor [%d][%d] on %s" % (tokens, heads_q, q.device))
+        pw, nw = None, 0
+        if ws is not None:
+            pw, nw = self._ws(ws)
+        else:
+            size = self.prompt_attend_workspace_bytes(tokens, heads_q, heads, D, batch)
+            if size:
+                ws = self._empty(q, (size + 256,), torch.uint8)
+                pw, nw = self._ws(ws)
+        rc = self._lib.etf_prompt_attend(self._h, ETF_KV_BF16 if dtype is torch.bfloat16 else ETF_KV_FP16, D, pq, sq, pk, sk, pv, sv, tokens, heads_q, heads,
+                                         starts.data_ptr(), batch, D ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), pw, nw)
+        if rc < 0:
+            self._ck(rc)
         return out
+
+    def _empty(self, like, shape, dtype):
+        """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
+        import torch
+        mine = self._stream or 0
+        if not like.is_cuda or _current_stream(like.get_device()) == mine:
+            return torch.empty(shape, dtype=dtype, device=like.device)
+        # torch takes a stream of its pool for a pointer of zero
+        with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=like.device) if mine else torch.cuda.default_stream(like.device)):
+            return torch.empty(shape, dtype=dtype, device=like.device)
 
     def probe_bandwidth(self, kind: int, a, b, nbytes: int):
         """One launch of a streaming probe kernel over the uint8 device tensors a and b (256-byte aligned)."""

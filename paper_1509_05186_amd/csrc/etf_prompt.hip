@@ -36,7 +36,7 @@ inline int64_t al256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
 // How a call is cut up, and where its workspace's arrays lie.
 struct PromptPlan {
-    int64_t tiles = 0, grid = 0, o_ml = 0, total = 256;  // tiles of one head that there can be
+    int64_t tiles = 0, grid = 0, o_ml = 0, total = 0;  // tiles of one head that there can be
     int ranges = 1, per = INT32_MAX;
 };
 
@@ -108,8 +108,8 @@ extern "C" int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const vo
     if (dtype != ETF_KV_BF16 && dtype != ETF_KV_FP16) return fail(ctx, ETF_EINVAL, "unknown type %d", dtype);
     if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, ETF_EINVAL, "scale must be positive and finite");
     if (!starts || !out || !aligned16(out)) return fail(ctx, ETF_EINVAL, "starts or out is null, or out not 16-byte aligned");
-    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(ctx, ETF_EINVAL, "workspace is null or not 256-byte aligned");
-    if (ws_bytes < p.total) return fail(ctx, ETF_ENOMEM, "workspace too small: %lld < %lld", (long long)ws_bytes, (long long)p.total);
+    if (p.total > 0 && (!ws || ((uintptr_t)ws & 255) != 0)) return fail(ctx, ETF_EINVAL, "workspace is null or not 256-byte aligned");
+    if (p.total > 0 && ws_bytes < p.total) return fail(ctx, ETF_ENOMEM, "workspace too small: %lld < %lld", (long long)ws_bytes, (long long)p.total);
     PromptArgs a{};
     if ((rc = check_packed(ctx, "q", q, q_strides, heads_q, head_dim, a.qs)) != ETF_OK) return rc;
     if ((rc = check_packed(ctx, "k", k, k_strides, heads, head_dim, a.ks)) != ETF_OK) return rc;
