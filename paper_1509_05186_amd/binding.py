@@ -215,7 +215,9 @@ def load_library():
 
 
 def _current_stream(gpu: int) -> int:
-    """torch's current stream on that GPU, as a number."""
+    """torch's current stream on that GPU, as a number; 0 for the CPU."""
+    if gpu < 0:
+        return 0
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # current_stream() without the object around it
     return raw(gpu) if raw is not None else torch.cuda.current_stream(gpu).cuda_stream
@@ -995,7 +997,7 @@ class Context:
         batch = starts.numel() - 1
         if batch < 1 or starts.dim() != 1 or starts.dtype != torch.int32 or not starts.is_contiguous() or starts.get_device() != gpu:
             raise ValueError("starts: expected a contiguous int32 tensor [B + 1] on %s, B at least 1" % q.device)
-        here = gpu < 0 or _current_stream(gpu) == (self._stream or 0)
+        here = _current_stream(gpu) == (self._stream or 0)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format) if here else self._empty(q, shape, dtype)
         elif out.shape != shape or out.dtype != dtype or not out.is_contiguous() or out.get_device() != gpu:
@@ -1020,7 +1022,7 @@ class Context:
         """A tensor of the stream that the context's work runs on: neither its earlier nor its later use there needs a wait."""
         import torch
         mine = self._stream or 0
-        if not like.is_cuda or _current_stream(like.get_device()) == mine:
+        if _current_stream(like.get_device()) == mine:
             return torch.empty(shape, dtype=dtype, device=like.device)
         # torch takes a stream of its pool for a pointer of zero
         with torch.cuda.stream(torch.cuda.ExternalStream(mine, device=like.device) if mine else torch.cuda.default_stream(like.device)):

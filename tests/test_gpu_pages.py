@@ -350,6 +350,81 @@ def test_served_from_packed_prompts_to_shared_pages():
     assert torch.equal(ctx.kv_attend(pool, q[[0, 1, 2, 0]].contiguous()), got)
 
 
+def test_a_draft_is_taken_back_after_a_fork():
+    """A block that others share already is completed again: it gets another page, and theirs stays as it is."""
+    say("draft after a fork")
+    T, H, D = BF, 2, 64
+    gen = torch.Generator().manual_seed(12)
+    ctx = context()
+    rand = lambda n: torch.randn(2, n, H, D, generator=gen).to(T).cuda()  # noqa: E731
+    pool = etf.KvCache.alloc(2, H, D, 256, dtype=T, pages=8)
+    refs = torch.zeros(8, dtype=torch.int32, device="cuda")
+    only = torch.tensor([60, 0], dtype=torch.int32, device="cuda")
+    ctx.kv_append(pool, rand(60), rand(60), counts=only)
+    pool.lens += only
+    draft = torch.tensor([10, 0], dtype=torch.int32, device="cuda")
+    assert int(ctx.kv_take(pool, refs, 10, counts=draft)) == 0
+    ctx.kv_append(pool, rand(10), rand(10), counts=draft)
+    pool.lens += draft
+    ctx.kv_fork(pool, refs, torch.tensor([0, 0], dtype=torch.int32, device="cuda"))
+    q = torch.randn(2, 1, 2 * H, D, generator=gen).to(T).cuda()
+    before = ctx.kv_attend(pool, q[[0, 0]].contiguous())
+    assert torch.equal(before[0], before[1]) and pool.lens.tolist() == [70, 70]
+    page = pool.table[1, :, 0].clone()
+    assert torch.equal(pool.table[0, :, 0], page) and (refs[page.long()] == 2).all()
+    # two of the ten were right; four others follow
+    pool.lens[0] -= 8
+    more = torch.tensor([4, 0], dtype=torch.int32, device="cuda")
+    assert int(ctx.kv_take(pool, refs, 4, counts=more)) == 0
+    assert (pool.table[0, :, 0] != page).all() and torch.equal(pool.table[1, :, 0], page) and (refs[page.long()] == 1).all()
+    ctx.kv_append(pool, rand(4), rand(4), counts=more)
+    pool.lens += more
+    after = ctx.kv_attend(pool, q[[0, 0]].contiguous())
+    assert pool.lens.tolist() == [66, 70] and torch.equal(after[1], before[1]) and not torch.equal(after[0], before[0])
+
+
+def test_pools_of_more_than_4_gib():
+    """Offsets of pages beyond 2^32 bytes."""
+    say("large pool")
+    pages, D = 540_000, 128     # 4.4 GB of keys
+    assert pages * 64 * D > 1 << 32
+    pool = etf.KvCache.alloc(1, 1, D, 64 * 3, pages=pages)
+    for i, p in enumerate((pages - 1, pages - 7)):
+        pool.k[p].view(torch.uint8).fill_(17 + i)
+        pool.v[p].view(torch.uint8).fill_(33 + i)
+        pool.bounds[p].view(torch.uint8).fill_(49 + i)
+        pool.scales[p].fill_(2.0 ** i)
+        pool.table[0, 0, i] = p
+    refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    refs[pool.table[0, 0, :2].long()] = 1
+    ctx = context()
+    pool.lens.fill_(130)
+    assert int(ctx.kv_take(pool, refs, 64)) == 0 and pool.table.tolist() == [[[pages - 1, pages - 7, 0]]]
+    used = ctx.kv_compact(pool, refs)
+    assert int(used) == 3 and pool.table.tolist() == [[[1, 2, 0]]] and refs[:4].tolist() == [1, 1, 1, 0] and int(refs.sum()) == 3
+    for i, p in enumerate((1, 2)):
+        assert (pool.k[p].view(torch.uint8) == 17 + i).all() and (pool.v[p].view(torch.uint8) == 33 + i).all() and (pool.bounds[p].view(torch.uint8) == 49 + i).all()
+        assert (pool.scales[p] == 2.0 ** i).all()
+
+
+def test_calls_on_another_stream_than_the_current_one():
+    say("another stream")
+    c, refs = a_cache([63, 130, 191, 0], 2, 64, 9, spare=60, shared=0.3)
+    want, after = pg.fork(c, refs, [1, 1, 0, 2])
+    table, after, lack = pg.take(want, after, 70)
+    want, after, many = pg.compact(dict(want, table=table), after)
+    ctx, cache, r = context(), on_gpu(c), refs.cuda()
+    src = torch.tensor([1, 1, 0, 2], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        ctx.kv_fork(cache, r, src)
+        missing = ctx.kv_take(cache, r, 70)
+        used = ctx.kv_compact(cache, r)
+    torch.cuda.synchronize()
+    same(cache, want, "another stream")
+    assert torch.equal(r.cpu(), after) and int(missing) == lack and int(used) == many
+
+
 def test_in_a_graph():
     """A step's calls captured and replayed, with eager calls on the same arrays between the replays."""
     say("graph")

@@ -154,7 +154,8 @@ def test_strides(D):
     # one key and value for all heads
     one = k[:, :1].expand(T, H, D)
     assert torch.equal(ctx.prompt_attend(q, one, one, starts), ctx.prompt_attend(q, one.contiguous(), one.contiguous(), starts))
-    check(prompt.attend(q.cpu(), k.cpu(), v.cpu(), starts.tolist(), D ** -0.5), want, torch.zeros(T, H * g).double() * 0 + prompt.attend(q.cpu(), k.cpu(), v.cpu(), starts.tolist(), D ** -0.5)["lse"], BF, "strides")
+    r = prompt.attend(q.cpu(), k.cpu(), v.cpu(), starts.tolist(), D ** -0.5)
+    check(r, want, r["lse"], BF, "strides")
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
@@ -253,3 +254,42 @@ def test_another_current_stream():
         out = ctx.prompt_attend(q, k, v, starts)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_rows_beyond_2_to_the_32():
+    """Many short prompts whose rows lie beyond 2^32 elements: the last ones as in a call of their own."""
+    say("far rows")
+    Hq, H, D, n, each = 32, 8, 128, 11_000, 96
+    T = n * each
+    assert T * Hq * D > 1 << 32
+    q = torch.zeros(T, Hq, D, dtype=BF, device="cuda")
+    k = torch.zeros(T, H, D, dtype=BF, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    last = 3 * each
+    q[-last:] = torch.randn(last, Hq, D, generator=gen, device="cuda").to(BF)
+    k[-last:] = torch.randn(last, H, D, generator=gen, device="cuda").to(BF)
+    ctx = context()
+    out = ctx.prompt_attend(q, k, k, torch.arange(0, T + 1, each, dtype=torch.int32, device="cuda"))
+    want = ctx.prompt_attend(q[-last:].clone(), k[-last:].clone(), k[-last:].clone(), torch.arange(0, last + 1, each, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out[-last:], want) and not want.isnan().any() and (out[: each * 10] == 0).all()
+
+
+def test_a_row_does_not_depend_on_the_rows_beside_it():
+    """The same prompt alone, and among others."""
+    say("alone and among others")
+    gen = torch.Generator().manual_seed(13)
+    q, k, v = (x.cuda() for x in rows(gen, HF, 700, 6, 2, 96))
+    ctx = context()
+    among = ctx.prompt_attend(q, k, v, torch.tensor([0, 37, 500, 700], dtype=torch.int32, device="cuda"))
+    alone = ctx.prompt_attend(q[37:500].clone(), k[37:500].clone(), v[37:500].clone(), torch.tensor([0, 463], dtype=torch.int32, device="cuda"))
+    assert torch.equal(among[37:500], alone)
+
+
+def test_gradients_are_refused():
+    gen = torch.Generator().manual_seed(14)
+    q, k, v = (x.cuda() for x in rows(gen, BF, 10, 2, 2, 64))
+    starts = torch.tensor([0, 10], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="gradient"):
+        context().prompt_attend(q.requires_grad_(), k, v, starts)
+    with torch.no_grad():
+        context().prompt_attend(q, k, v, starts)
