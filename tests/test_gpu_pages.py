@@ -466,3 +466,18 @@ def test_in_a_graph():
             step()
             side.synchronize()
             same(cache, want, "eager %d" % i)
+
+
+def test_example_of_shared_prompts():
+    say("example")
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "shared_prompts.py")
+    spec = importlib.util.spec_from_file_location("shared_prompts", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for args in (["--batch", "6", "--heads", "2", "--shared", "333", "--own", "90", "--tokens", "70", "--head-dim", "64"], ["--batch", "1", "--heads", "1", "--group", "3", "--shared", "64", "--own", "1", "--tokens", "1"]):
+        cache, refs, used, off = example.main(args)
+        assert off < 0.02       # outputs of some 0.2 in size, a step of bfloat16 each
+        c = {name: getattr(cache, name).cpu() for name in etf.KvCache.FIELDS}
+        assert torch.equal(pg.count(c), refs.cpu()) and (refs[:used] > 0).all() and not refs[used:].any()
