@@ -478,6 +478,8 @@ def test_example_of_shared_prompts():
     spec.loader.exec_module(example)
     for args in (["--batch", "6", "--heads", "2", "--shared", "333", "--own", "90", "--tokens", "70", "--head-dim", "64"], ["--batch", "1", "--heads", "1", "--group", "3", "--shared", "64", "--own", "1", "--tokens", "1"]):
         cache, refs, used, off = example.main(args)
-        assert off < 0.02       # outputs of some 0.2 in size, a step of bfloat16 each
+        # off by the roundings of bf16 only: those of the weights and of the output
+        most = float(cache.tail_v.abs().max().clamp_min(448 * cache.scales[:, 1].max()))
+        assert off <= 2 * 2.0 ** -8 * most + 2.0 ** -12 * most
         c = {name: getattr(cache, name).cpu() for name in etf.KvCache.FIELDS}
         assert torch.equal(pg.count(c), refs.cpu()) and (refs[:used] > 0).all() and not refs[used:].any()
