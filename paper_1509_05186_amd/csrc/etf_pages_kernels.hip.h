@@ -172,7 +172,8 @@ __device__ __forceinline__ Ranks ranks_of(const Flags &f, int *s_upto, int *s_su
 // Take.  Slots are the blocks that an append of n tokens may complete, `per` of every (sequence, head): slot (b, h, c) is block
 // lens[b] / 64 + c.  A slot that the sequence's own count completes wants a page unless it has one that no other entry names.  The
 // wanting slots get the lowest free pages, in their order.
-// Two launches, each as long as its chain of dependent loads.
+// Two launches, each a chain of dependent loads: 512 slots and 24 588 pages 3.8 and 2.3 us, 32 768 slots (22 290 of them wanting) and 438 616 pages 5.3 and
+// 6.7 us (13 with 1024 slots to a workgroup).
 // ------------------------------------------------------------------------------------------------
 struct TakeArgs {
     PageView c;
@@ -257,7 +258,9 @@ __global__ __launch_bounds__(256) void k_kv_take(TakeArgs a)
 // ------------------------------------------------------------------------------------------------
 // Compact.  With U pages in use, the i-th of the others below U takes the used page that has i used ones behind it.  All of that
 // follows from the ranks, so one launch after the flags moves the pages (sources lie from U on, destinations below), and
-// rewrites the table and refs.  Bound by the pages' bytes, read once and written once.
+// rewrites the table and refs.  Bound by the pages' bytes, read once and written once: 547 MB in 118 us = 4.6 TB/s (a plain copy's 5.1), 95 us = 5.8 TB/s
+// where the pool was moved just before.  Pages are spread over as many workgroups as the card holds (2048) before one takes a second, 16 at a time
+// at most: the ranks of 16 are found side by side.
 // ------------------------------------------------------------------------------------------------
 struct CompactArgs {
     PageView c;
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(256) void k_kv_used_flags(CompactArgs a)
     put_flags(a.taken, blockIdx.x, s_sum, [&](int64_t i) { return a.refs[i] > 0; });
 }
 
-// 64 x D bytes
+// 64 x D bytes, past the caches: 118 us where plain loads and stores take 123 (compact, 16 396 pages of 128 dimensions moved)
 template <int D>
 __device__ __forceinline__ void move_page(uint8_t *of, int64_t to, int64_t from, int tid)
 {
@@ -282,7 +285,7 @@ __device__ __forceinline__ void move_page(uint8_t *of, int64_t to, int64_t from,
     u32x4 w[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-        if (PIECES % 256 == 0 || tid + 256 * i < PIECES) w[i] = reinterpret_cast<const u32x4 *>(of + from * (PAGE_KB * D))[tid + 256 * i];
+        if (PIECES % 256 == 0 || tid + 256 * i < PIECES) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(of + from * (PAGE_KB * D)) + tid + 256 * i);
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
         if (PIECES % 256 == 0 || tid + 256 * i < PIECES) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4 *>(of + to * (PAGE_KB * D)) + tid + 256 * i);
@@ -340,7 +343,7 @@ __global__ __launch_bounds__(256) void k_kv_compact(CompactArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------
-// Free: one share less of each listed page, none below zero.
+// Free: one share less of each listed page, none below zero.  3.9 us for 40 448 entries, of which 8192 are pages: a load, an atomic that returns, another.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_kv_free(int32_t *refs, int pages, const int32_t *list, int64_t n)
 {
@@ -358,7 +361,8 @@ __global__ __launch_bounds__(256) void k_kv_free(int32_t *refs, int pages, const
 // ------------------------------------------------------------------------------------------------
 // Fork.  The first launch decides what happens to every sequence and saves the rows of those sources that do not stay as they are
 // themselves; the second writes every changed sequence's row, open block and lengths, and counts shares: one less for every entry that
-// was there, one more for every entry that is.
+// was there, one more for every entry that is.  32 sequences of 8 heads, 16 of them copied: 2.3 and 4.2 us (5.2 with a row's table, keys
+// and values by one workgroup), chains of dependent loads.
 // ------------------------------------------------------------------------------------------------
 enum { FORK_STAYS = 0, FORK_COPY = 1, FORK_SAVED = 2, FORK_CUT = 3, FORK_EMPTY = 4 };
 struct ForkArgs {

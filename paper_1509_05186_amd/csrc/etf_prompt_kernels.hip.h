@@ -21,7 +21,15 @@ struct PromptArgs {
 // maximum and sum are the lane's own (and its neighbour's 32 lanes up), and p^T stands in its registers as the second product wants
 // it: of 16 tokens, those 8 (j / 4) + 4 (lane / 32) + j % 4.  Blocks of 64 tokens go straight from memory to LDS, the next one while this
 // one is worked on; values are read transposed (ds_read_b64_tr_b16: 16 lanes exchange 4 x 4 numbers).  Pieces of 16 bytes are
-// exchanged within a row of LDS, so that lanes that read together hit all banks.
+// exchanged within a row of LDS, so that lanes that read together hit all banks (no conflicts are counted).  A weight is rounded to the rows' type
+// for its product, as in k_kv_attend; its sum takes it unrounded.
+// Bound by the power that the card has for it: it runs at 1.9 GHz of 2.4, at which the matrix cores are busy 48 % of the time and vector issue 45 % (128
+// dimensions; 64: 49 % and 77 %, the exponentials).  Two prompts of 4096 tokens, 32 heads of 128 dimensions: 281 to 290 us = 950 to 980 TFLOP/s, where a matrix product
+// of 8192^3 reaches 1230.  One prompt of 8192, 64 dimensions: 305 us = 900 TFLOP/s; 34 356 tokens in 24 prompts of 1 to 2500, five query heads of 96
+// dimensions to each: 305 us = 770 TFLOP/s.  Tried for the first of these, 289 us at that time: the next block's first product and the block before's second one between the
+// exponentials 484 (registers: one wave to a unit); 64 rows a wave 403 (likewise); eight waves of which four multiply while four take exponentials 304 to 366;
+// loads into LDS spread between the products 298 to 312; values transposed on their way into LDS and read 16 bytes at a time 311; wave priorities 300 to 310;
+// maxima only where a sum of weights asks for them 854 (registers).
 // ------------------------------------------------------------------------------------------------
 // 16 bytes to a lane from offset `at` of the `bytes` bytes at `from` (nothing is read behind them) to the 1 KB of LDS at `to`, in the
 // order of the lanes.  `from`, `bytes` and `to` are the same for all lanes.
