@@ -660,7 +660,7 @@ enum {
     ETF_K_IVF_COARSE = 11, /* IVFADC: distances to the centroids and probe selection */
     ETF_K_IVF_SCAN = 12,   /* IVFADC: scan of the probed lists                        */
     ETF_K_LDS16 = 13,      /* tree / forest candidate filter on 16-bit tables in LDS  */
-    ETF_K_KV = 14,         /* attention over a cache in 8 bits: append, attend, select, evict */
+    ETF_K_KV = 14,         /* attention over a cache in 8 bits, its pages, attention of prompts */
     ETF_K_COUNT = 15
 };
 /* on != 0: every later kernel launch of this context is bracketed by a pair of

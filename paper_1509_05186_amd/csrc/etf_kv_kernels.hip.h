@@ -44,9 +44,9 @@ __device__ __forceinline__ int64_t kv_tail(const KvView &c, int64_t bh, int b, i
 // lie in the same buffer: everything is read before anything is written.  Values of an open block lie by dimensions: eight tokens
 // to a load, and turned in LDS to a store where eight are left over.  A token that is not finite has keys that are not numbers
 // and values of zero: rows that see it become not a number, others do not.
-// Bound by vector issue and memory alike: four prompts of 8192 tokens, 8 heads of 128 dimensions (202 MB) 45 us = 4.5 TB/s; with maxima and
-// bounds number by number instead of two to an operation 53 us.  Packed prompts of 1366 to 4096 tokens (269 MB) 54 us = 5.0 TB/s.  Short calls are a chain
-// of dependent steps: one token 2.2 us (with barriers and LDS 3.1), a block 6.0, a block of which 60 tokens were open and 60 are left over 9.9 (11.6 with the open
+// Bound by vector issue and memory alike: four prompts of 8192 tokens, 8 heads of 128 dimensions (202 MB) 45 to 48 us = 4.2 to 4.5 TB/s; with maxima and
+// bounds number by number instead of two to an operation 53 us.  Packed prompts of 1617 to 4096 tokens (269 MB) 54 us = 5.0 TB/s, 63 with other
+// tensors each time.  Short calls are a chain of dependent steps: one token 2.2 us (with barriers and LDS 3.1), a block 6.0, a block of which 60 tokens were open and 60 are left over 9.9 (11.6 with the open
 // block's values read two bytes at a time and what is left over read twice).
 // ------------------------------------------------------------------------------------------------
 struct KvAppendArgs {
