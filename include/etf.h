@@ -632,8 +632,8 @@ int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs,
  *           aligned.  Query head x reads key/value head x / (heads_q / heads)
  *   starts  i32 [batch + 1], device, ascending, within [0, tokens]; counts as 0 or as tokens outside of that.  A sequence of no tokens, or
  *           whose end lies before its start, has no rows
- *   out     dense [tokens][heads_q][head_dim], the rows' type; lse: NULL or float [tokens][heads_q].  Rows of tokens that
- *           are no sequence's are left as they were
+ *   out     dense [tokens][heads_q][head_dim], the rows' type; lse: NULL or float [tokens][heads_q].  Both share nothing with q, k, v.
+ *           Rows of tokens that are no sequence's are left as they were
  *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes; any where that is 0
  * A row whose query, or of which a key that it sees, makes a logit +inf or not a number becomes not a number; a value that is not finite
  * makes its dimension so, in the rows that see it and in no other. */

@@ -468,6 +468,93 @@ def test_in_a_graph():
             same(cache, want, "eager %d" % i)
 
 
+def test_append_packed_and_free_on_another_stream_and_in_a_graph():
+    """Captured and replayed, with eager calls on the same arrays between the replays; the shares of pages that are listed more than once."""
+    say("append packed, free: streams, graph")
+    T, H, D, lens, counts = HF, 2, 96, [60, 0, 130], [70, 64, 3]
+    gen = torch.Generator().manual_seed(31)
+    c = kv.new_cache(3, H, D, 4, T)
+    kv.append(c, *(torch.randn(3, 130, H, D, generator=gen).to(T) for _ in range(2)), torch.tensor(lens))
+    c["lens"].copy_(torch.tensor(lens))
+    starts = starts_of(counts)
+    k, v = (torch.randn(starts[-1], H, D, generator=gen).to(T) for _ in range(2))
+    padded = [torch.zeros(3, 70, H, D, dtype=T) for _ in range(2)]
+    for b, n in enumerate(counts):
+        padded[0][b, :n], padded[1][b, :n] = k[starts[b] : starts[b] + n], v[starts[b] : starts[b] + n]
+    before = {name: c[name].clone() for name in etf.KvCache.FIELDS}
+    kv.append(c, *padded, torch.tensor(counts))
+    refs0 = torch.tensor([3, 1, 0, 2, 5], dtype=torch.int32)
+    listed = torch.tensor([0, 0, -1, 1, 1, 2, 3, 9, 4, 0, 0], dtype=torch.int32)
+    want = torch.tensor([0, 0, 0, 1, 4], dtype=torch.int32)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        kg, vg, st, lg, refs = k.cuda(), v.cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), listed.cuda(), refs0.cuda()
+        cache = on_gpu(before)
+        ctx = etf.Context(device=0, stream=side.cuda_stream)
+        side.synchronize()
+
+        def step():
+            ctx.kv_append_packed(cache, kg, vg, st)
+            ctx.kv_free(refs, lg)
+
+        def restore():
+            for name in etf.KvCache.FIELDS:
+                getattr(cache, name).copy_(before[name])
+            refs.copy_(refs0)
+
+        def right(what):
+            side.synchronize()
+            for name in etf.KvCache.FIELDS:
+                x, y = getattr(cache, name).cpu().float(), c[name].float()
+                assert torch.equal(x, y), "%s: %s" % (what, name)
+            assert torch.equal(refs.cpu(), want), what
+
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for i in range(3):
+            restore()
+            graph.replay()
+            right("replay %d" % i)
+            restore()
+            step()
+            right("eager %d" % i)
+        restore()
+    side.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        step()
+    right("another current stream")
+
+
+def test_append_packed_of_tokens_beyond_2_to_the_32():
+    """Keys and values that lie beyond 2^32 elements, of tokens of which most are no sequence's."""
+    say("append packed: far tokens")
+    H, D = 8, 128
+    tokens = (1 << 32) // (H * D) + 4321
+    k = torch.zeros(tokens, H, D, dtype=BF, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    k[-300:] = torch.randn(300, H, D, generator=gen, device="cuda").to(BF)
+    assert (tokens - 300) * H * D > 1 << 32
+    ctx = context()
+    far, near = (etf.KvCache.alloc(3, H, D, 256, dtype=BF) for _ in range(2))
+    starts = torch.tensor([0, 130, 130, 300], dtype=torch.int32, device="cuda")
+    ctx.kv_append_packed(far, k, k, starts + (tokens - 300))
+    few = k[-300:].clone()
+    ctx.kv_append_packed(near, few, few, starts)
+    torch.cuda.synchronize()
+    full = torch.tensor([2, 0, 2])
+    for b in range(3):
+        n = int(full[b])
+        for h in range(H):
+            for p in near.table[b, h, :n].tolist():
+                for name in ("k", "v", "bounds"):
+                    assert torch.equal(getattr(far, name)[p].view(torch.uint8), getattr(near, name)[p].view(torch.uint8)), (b, h, name)
+                assert torch.equal(far.scales[p], near.scales[p])
+    same_open = [torch.equal(far.tail_k[b, :, 0, : m], near.tail_k[b, :, 0, : m]) and torch.equal(far.tail_v[b, :, 0, :, : m], near.tail_v[b, :, 0, :, : m]) for b, m in ((0, 2), (2, 42))]
+    assert all(same_open)
+    assert torch.equal(near.tail_k[2, :, 0, :42].transpose(0, 1), few[258:]) and torch.equal(near.tail_k[0, :, 0, :2].transpose(0, 1), few[128:130])
+
+
 def test_example_of_shared_prompts():
     say("example")
     import importlib.util

@@ -285,6 +285,82 @@ def test_a_row_does_not_depend_on_the_rows_beside_it():
     assert torch.equal(among[37:500], alone)
 
 
+def test_ranges_on_another_stream_and_in_a_graph():
+    """With a workspace: the library's own on a stream that is not the current one, one taken while the graph is captured, and the caller's."""
+    say("ranges, streams, graph")
+    gen = torch.Generator().manual_seed(21)
+    lens = [1500, 700]
+    q, k, v = (x.cuda() for x in rows(gen, HF, sum(lens), 2, 1, 64))
+    starts = torch.tensor(starts_of(lens), dtype=torch.int32, device="cuda")
+    need = context().prompt_attend_workspace_bytes(sum(lens), 2, 1, 64, 2)
+    assert need > 0
+    want = context().prompt_attend(q, k, v, starts)
+    torch.cuda.synchronize()
+    ctx = context()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        out = ctx.prompt_attend(q, k, v, starts)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = etf.Context(device=0, stream=side.cuda_stream)
+        for room in (None, torch.empty(need + 256, dtype=torch.uint8, device="cuda")):
+            out = torch.empty_like(q)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                ctx.prompt_attend(q, k, v, starts, out=out, ws=room)
+            for _ in range(3):
+                out.fill_(0)
+                graph.replay()
+                eager = ctx.prompt_attend(q, k, v, starts)
+                side.synchronize()
+                assert torch.equal(out, want) and torch.equal(eager, want)
+
+
+def test_two_calls_at_once():
+    """Two contexts on streams of their own, with ranges and without."""
+    say("two at once")
+    gen = torch.Generator().manual_seed(22)
+    work = []
+    for lens, dtype, D in (([1500, 700], HF, 64), ([40, 0, 900], BF, 128)):
+        x = [t.cuda() for t in rows(gen, dtype, sum(lens), 2, 1, D)] + [torch.tensor(starts_of(lens), dtype=torch.int32, device="cuda")]
+        work.append((x, context().prompt_attend(*x)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    ctxs = [etf.Context(device=0, stream=s.cuda_stream) for s in streams]
+    outs = []
+    for _ in range(10):
+        for (x, _), s, ctx in zip(work, streams, ctxs):
+            with torch.cuda.stream(s):
+                outs.append(ctx.prompt_attend(*x))
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        assert torch.equal(out, work[i % 2][1]), i
+
+
+@pytest.mark.parametrize("dtype,D,T", [(BF, 64, 70_001), (HF, 128, 66_000)])
+def test_one_long_prompt(dtype, D, T):
+    """Tens of thousands of tokens: some rows of it, each over what it sees, in float64."""
+    say("long", dtype, D, T)
+    gen = torch.Generator().manual_seed(23)
+    q, k, v = rows(gen, dtype, T, 2, 1, D)
+    out, lse = run(q, k, v, [0, T])
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    at = [0, 1, 63, 64, 4095, 33_333, T - 66, T - 2, T - 1]
+    r = {name: [] for name in ("out", "lse", "size", "reach", "mag", "seen", "vmax")}
+    kk, vv, scale = k[:, 0].double(), v[:, 0].double(), D ** -0.5
+    for i in at:
+        s = q[i].double() @ kk[: i + 1].T * scale
+        lse_i = torch.logsumexp(s, 1)
+        p = torch.exp(s - lse_i[:, None])
+        for name, x in (("out", p @ vv[: i + 1]), ("lse", lse_i), ("size", p @ vv[: i + 1].abs()), ("reach", s.abs().amax(1)),
+                        ("mag", (q[i].double().abs() @ kk[: i + 1].abs().T * scale).amax(1)), ("seen", torch.full((2,), i + 1.0, dtype=torch.float64)),
+                        ("vmax", vv[: i + 1].abs().max().expand(2))):
+            r[name].append(x)
+    check({name: torch.stack(x) for name, x in r.items()}, out.cpu()[at], lse.cpu()[at], dtype, "long")
+
+
 def test_gradients_are_refused():
     gen = torch.Generator().manual_seed(14)
     q, k, v = (x.cuda() for x in rows(gen, BF, 10, 2, 2, 64))
