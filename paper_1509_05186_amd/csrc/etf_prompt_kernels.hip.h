@@ -29,7 +29,8 @@ struct PromptArgs {
 // dimensions to each: 305 us = 770 TFLOP/s.  Tried for the first of these, 289 us at that time: the next block's first product and the block before's second one between the
 // exponentials 484 (registers: one wave to a unit); 64 rows a wave 403 (likewise); eight waves of which four multiply while four take exponentials 304 to 366;
 // loads into LDS spread between the products 298 to 312; values transposed on their way into LDS and read 16 bytes at a time 311; wave priorities 300 to 310;
-// maxima only where a sum of weights asks for them 854 (registers).
+// maxima only where a sum of weights asks for them 854 (registers); half of a wave's last block left out where it sees no more than the other, 293 -> 311, and 314 -> 353 for
+// the 24 prompts (registers: 162 -> 197 with 96 dimensions).
 // ------------------------------------------------------------------------------------------------
 // 16 bytes to a lane from offset `at` of the `bytes` bytes at `from` (nothing is read behind them) to the 1 KB of LDS at `to`, in the
 // order of the lanes.  `from`, `bytes` and `to` are the same for all lanes.
