@@ -81,8 +81,9 @@ def kernel_source_hash():
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_1509_05186_amd", "csrc")
     for name in sorted(os.listdir(csrc)):
-        # what the profiled kernels are compiled from; host-only .cpp files and the attention cache's kernels do not move a profile
-        if name.endswith((".hip", ".h")) and not name.startswith("etf_kv"):
+        # what the profiled kernels are compiled from; host-only .cpp files and the attention's kernels (the cache, its pages, prompts) do
+        # not move a profile
+        if name.endswith((".hip", ".h")) and not name.startswith(("etf_kv", "etf_pages", "etf_prompt")):
             h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()[:16]
 

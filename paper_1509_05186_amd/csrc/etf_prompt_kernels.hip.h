@@ -24,9 +24,9 @@ struct PromptArgs {
 // exchanged within a row of LDS, so that lanes that read together hit all banks (no conflicts are counted).  A weight is rounded to the rows' type
 // for its product, as in k_kv_attend; its sum takes it unrounded.
 // Bound by the clock, which falls to 1.9 GHz of 2.4 under it, and by phases that wait for each other: the matrix cores are busy 52 % of the time and vector issue 50 % (128
-// dimensions; 64: 49 % and 79 %, the exponentials).  Two prompts of 4096 tokens, 32 heads of 128 dimensions: 281 to 290 us = 950 to 980 TFLOP/s, where a matrix product
-// of 8192^3 reaches 1230.  One prompt of 8192, 64 dimensions: 305 us = 900 TFLOP/s; 34 356 tokens in 24 prompts of 1 to 2500, five query heads of 96
-// dimensions to each: 305 us = 770 TFLOP/s.  Tried for the first of these, 289 us at that time: the next block's first product and the block before's second one between the
+// dimensions; 64: 49 % and 79 %, the exponentials).  Two prompts of 4096 tokens, 32 heads of 128 dimensions: 279 to 293 us = 940 to 985 TFLOP/s, where a matrix product
+// of 8192^3 reaches 1230.  One prompt of 8192, 64 dimensions: 298 to 318 us = 865 to 920 TFLOP/s; 34 356 tokens in 24 prompts of 1 to 2500, five query heads of 96
+// dimensions to each: 305 to 315 us = 750 to 775 TFLOP/s.  Tried for the first of these, 289 us at that time: the next block's first product and the block before's second one between the
 // exponentials 484 (registers: one wave to a unit); 64 rows a wave 403 (likewise); eight waves of which four multiply while four take exponentials 304 to 366;
 // loads into LDS spread between the products 298 to 312; values transposed on their way into LDS and read 16 bytes at a time 311; wave priorities 300 to 310;
 // maxima only where a sum of weights asks for them 854 (registers); half of a wave's last block left out where it sees no more than the other, 293 -> 311, and 314 -> 353 for
