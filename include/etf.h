@@ -584,14 +584,20 @@ int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void *q, const 
  * <= budget) and those of the others with the largest mass (float [batch][heads][max_blocks]; ties to the lower block, what is
  * not a number last) stay, in their order; the open block stays too.  table_out, mass_out (entries past the full blocks: -1;
  * the open block's weight, then 0), lens_out and evicted_out [batch] may be the arrays they are read from (up to
- * 16384 blocks a row), or others that share nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1. */
+ * 16384 blocks a row), or others that share nothing with them.  freed (i32 [batch][heads][max_blocks]): the pages that were taken out, then -1.
+ * Pages that entries past the full blocks name stand in neither afterwards: where their shares are counted (below), call _ahead. */
 int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
                  int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
+/* The same, but entries past the full blocks (pages that etf_kv_take has given ahead of their tokens, or of a draft that was taken back)
+ * stay in their order: the first of them is then the entry after the blocks that stay, and -1 follow the last. */
+int etf_kv_evict_ahead(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                       int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed);
 
 /* Pages.  refs (i32 [pages], the caller's) holds how many entries of the table name each page; a page with none (0 or less) is free.  Pages
  * of full blocks may be shared, by several sequences or by a table and what the caller keeps for later (one share each): the calls above
  * read them, and write only to those of blocks that an append completes, which etf_kv_take gives pages of their own.  A table
- * starts out with -1 throughout and refs with 0 (or with a page for every block, and refs with 1).
+ * starts out with -1 throughout and refs with 0 (or with a page for every block, and refs with 1).  Blocks are taken out of such a table
+ * by etf_kv_evict_ahead, which drops no entry that refs counts: what is in freed goes to etf_kv_free.
  *
  * etf_kv_take, ahead of etf_kv_append: every block that an append of counts tokens (i32 [batch]; NULL: all n) completes gets the lowest free
  * page, in the order (sequence, head, block), unless it has one that no other entry names; one that it shares loses that share.
@@ -610,7 +616,7 @@ int etf_kv_take(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs, in
 int64_t etf_kv_fork_workspace_bytes(const etf_ctx *ctx, const etf_kv_cache *cache);
 int etf_kv_fork(etf_ctx *ctx, const etf_kv_cache *cache, int32_t *refs, const int32_t *source, const int32_t *keep, void *ws, int64_t ws_bytes);
 
-/* One share less for each entry of list (i32 [n], device; etf_kv_evict's freed) that is a page of [0, pages), none below 0. */
+/* One share less for each entry of list (i32 [n], device; etf_kv_evict_ahead's freed) that is a page of [0, pages), none below 0. */
 int etf_kv_free(etf_ctx *ctx, int32_t *refs, int pages, const int32_t *list, int64_t n);
 
 /* Brings the pages that are in use, U of them, to [0, U): the i-th free one below U takes what is in the used one that has i used ones behind

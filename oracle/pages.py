@@ -4,6 +4,8 @@ A cache is a dict of CPU tensors as in oracle/kvcache.py, refs an int32 tensor. 
 """
 import torch
 
+from . import kvcache
+
 BLOCK = 64
 
 
@@ -80,6 +82,18 @@ def free(refs, pages):
         if 0 <= p < len(refs) and after[p] > 0:
             after[p] -= 1
     return after
+
+
+def evict(c, mass, budget, sink, recent):
+    """(table, lens, evicted, mass, freed) after an eviction that keeps the entries past the full blocks."""
+    table, lens, evicted, kept, freed = kvcache.evict(c, mass, budget, sink, recent)
+    blocks = table.shape[2]
+    for b in range(table.shape[0]):
+        full, stay = _len(c, b) // BLOCK, min(_len(c, b) // BLOCK, budget)
+        for h in range(table.shape[1]):
+            for j in range(full, blocks):
+                table[b, h, stay + j - full] = c["table"][b, h, j]
+    return table, lens, evicted, kept, freed
 
 
 def compact(c, refs):

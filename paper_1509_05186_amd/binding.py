@@ -28,7 +28,7 @@ EXPORTS = [
     "etf_profile_enable", "etf_profile_read", "etf_probe_bandwidth",
     "etf_ivf_set_coarse", "etf_ivf_assign_workspace_bytes", "etf_ivf_assign_device", "etf_ivf_build", "etf_ivf_stats",
     "etf_ivf_device_bytes", "etf_ivf_upload", "etf_ivf_workspace_bytes", "etf_ivf_search",
-    "etf_kv_append", "etf_kv_attend_workspace_bytes", "etf_kv_attend", "etf_kv_select_workspace_bytes", "etf_kv_select", "etf_kv_evict",
+    "etf_kv_append", "etf_kv_attend_workspace_bytes", "etf_kv_attend", "etf_kv_select_workspace_bytes", "etf_kv_select", "etf_kv_evict", "etf_kv_evict_ahead",
     "etf_kv_append_packed", "etf_kv_take_workspace_bytes", "etf_kv_take", "etf_kv_fork_workspace_bytes", "etf_kv_fork", "etf_kv_free",
     "etf_kv_compact_workspace_bytes", "etf_kv_compact",
     "etf_prompt_attend_workspace_bytes", "etf_prompt_attend",
@@ -196,6 +196,7 @@ def load_library():
         "etf_kv_select_workspace_bytes": (L, [P, P, I, I, I]),
         "etf_kv_select": (I, [P, P, P, P, I, I, P, I, I, I, P, P, L]),
         "etf_kv_evict": (I, [P, P, P, I, I, I, P, P, P, P, P]),
+        "etf_kv_evict_ahead": (I, [P, P, P, I, I, I, P, P, P, P, P]),
         "etf_kv_append_packed": (I, [P, P, P, P, P, P, L, P]),
         "etf_kv_take_workspace_bytes": (L, [P, P, I]),
         "etf_kv_take": (I, [P, P, P, I, P, P, P, P, P, L]),
@@ -839,9 +840,12 @@ class Context:
         self._ck(self._lib.etf_kv_select(self._h, cache._ref, pq, sq, n, heads_q, pc, w, sink, recent, pl, pw, nw))
         return lists
 
-    def kv_evict(self, cache: KvCache, mass, budget: int, sink: int = 0, recent: int = 0, to: Optional[KvCache] = None, mass_out=None, freed=None):
+    def kv_evict(self, cache: KvCache, mass, budget: int, sink: int = 0, recent: int = 0, to: Optional[KvCache] = None, mass_out=None, freed=None,
+                 ahead: bool = False):
         """Cuts every sequence's cache to `budget` full blocks by mass; returns (mass of what stays, pages taken out).  to: the
-        cache (fork()) whose table, lens and evicted are written; None: this one's, and mass is written over."""
+        cache (fork()) whose table, lens and evicted are written; None: this one's, and mass is written over.  Entries past the
+        full blocks become -1, or, with ahead, stay behind the blocks that stay: pages that kv_take has given ahead of their
+        tokens would else be in use for good (a cache whose pages are counted wants ahead=True)."""
         import torch
         self._kv_here(cache)
         blocks = (cache.batch, cache.heads, cache.max_blocks)
@@ -855,7 +859,8 @@ class Context:
         po = self._kv_dev(mass_out, blocks, torch.float32, cache, "mass_out")
         pf = self._kv_dev(freed, blocks, torch.int32, cache, "freed")
         c = (cache if to is None else to)._c
-        self._ck(self._lib.etf_kv_evict(self._h, cache._ref, pm, budget, sink, recent, c.table, c.lens, c.evicted, po, pf))
+        call = self._lib.etf_kv_evict_ahead if ahead else self._lib.etf_kv_evict
+        self._ck(call(self._h, cache._ref, pm, budget, sink, recent, c.table, c.lens, c.evicted, po, pf))
         return mass_out, freed
 
     def kv_append_packed(self, cache: KvCache, k, v, starts):
@@ -925,7 +930,7 @@ class Context:
         self._ck(self._lib.etf_kv_fork(self._h, cache._ref, pr, ps, pk, pw, nw))
 
     def kv_free(self, refs, pages):
-        """One share less in refs (int32 [pages of the pool]) for each page of the int32 tensor pages (kv_evict's freed), entries of -1 aside."""
+        """One share less in refs (int32 [pages of the pool]) for each page of the int32 tensor pages (the freed of kv_evict(ahead=True)), entries of -1 aside."""
         import torch
         gpu = refs.get_device()
         if gpu != self._device and self._device is not None:

@@ -377,8 +377,8 @@ extern "C" int etf_kv_select(etf_ctx *ctx, const etf_kv_cache *cache, const void
     });
 }
 
-extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
-                            int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed)
+static int evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out, int32_t *lens_out,
+                 int32_t *evicted_out, float *mass_out, int32_t *freed, bool ahead)
 {
     int rc = check_cache(ctx, cache, true);
     if (rc != ETF_OK) return rc;
@@ -397,18 +397,30 @@ extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float
     const bool apart = lens_out != cache->lens && evicted_out != cache->evicted && lens_out != cache->evicted && evicted_out != cache->lens;
     int32_t *lens = apart ? lens_out : nullptr;
     if (cache->max_blocks <= 256)
-        hipLaunchKernelGGL((k_kv_evict<1, 4>), grid, dim3(64), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+        hipLaunchKernelGGL((k_kv_evict<1, 4>), grid, dim3(64), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out, ahead);
     else if (cache->max_blocks <= 1024)
-        hipLaunchKernelGGL((k_kv_evict<4, 4>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+        hipLaunchKernelGGL((k_kv_evict<4, 4>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out, ahead);
     else if (cache->max_blocks <= 4096)
-        hipLaunchKernelGGL((k_kv_evict<4, 16>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+        hipLaunchKernelGGL((k_kv_evict<4, 16>), grid, dim3(256), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out, ahead);
     else if (cache->max_blocks <= KV_EVICT_MOST)
-        hipLaunchKernelGGL((k_kv_evict<16, 16>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+        hipLaunchKernelGGL((k_kv_evict<16, 16>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out, ahead);
     else
-        hipLaunchKernelGGL((k_kv_evict<16, 0>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out);
+        hipLaunchKernelGGL((k_kv_evict<16, 0>), grid, dim3(1024), 0, st, c, mass, budget, sink, recent, table_out, mass_out, freed, lens, evicted_out, ahead);
     LAUNCH_CHECK(ctx, "k_kv_evict");
     if (apart) return ETF_OK;
     hipLaunchKernelGGL(k_kv_evict_lens, dim3((unsigned)((cache->batch + 63) / 64)), dim3(64), 0, st, c, budget, lens_out, evicted_out);
     LAUNCH_CHECK(ctx, "k_kv_evict_lens");
     return ETF_OK;
+}
+
+extern "C" int etf_kv_evict(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                            int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed)
+{
+    return evict(ctx, cache, mass, budget, sink, recent, table_out, lens_out, evicted_out, mass_out, freed, false);
+}
+
+extern "C" int etf_kv_evict_ahead(etf_ctx *ctx, const etf_kv_cache *cache, const float *mass, int budget, int sink, int recent, int32_t *table_out,
+                                  int32_t *lens_out, int32_t *evicted_out, float *mass_out, int32_t *freed)
+{
+    return evict(ctx, cache, mass, budget, sink, recent, table_out, lens_out, evicted_out, mass_out, freed, true);
 }

@@ -1967,14 +1967,15 @@ __global__ __launch_bounds__(64 * ROWS * WAVES) void k_kv_pick(KvSelectArgs a)
 // ------------------------------------------------------------------------------------------------
 // Eviction: of every (sequence, head) with more than `budget` blocks the first `sink`, the last `recent` and those of
 // the others with the largest weight stay, in their order.  Lengths that are changed in place change in a launch of their own
-// (k_kv_evict_lens), since every workgroup here reads them; into other arrays (lens_out not null) they are written here.
+// (k_kv_evict_lens), since every workgroup here reads them; into other arrays (lens_out not null) they are written here.  With `ahead` the
+// entries behind the full blocks move down behind the blocks that stay: their pages would be lost to who counts shares.
 // Bound by latency: 7 us for 128 rows of 128 blocks, 10 for 16 rows of 313.
 // ------------------------------------------------------------------------------------------------
 // Everything is read before anything is written, since the outputs may be the inputs; with more blocks than the registers hold a launch
 // of one workgroup per row has to write apart from what it reads (KPT = 0: `table_out` and `mass_out` are not the inputs).
 template <int WAVES, int KPT>
 __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *mass, int budget, int sink, int recent, int32_t *table_out, float *mass_out,
-                                                         int32_t *freed, int32_t *lens_out, int32_t *evicted_out)
+                                                         int32_t *freed, int32_t *lens_out, int32_t *evicted_out, bool ahead)
 {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / c.heads), tid = threadIdx.x;
@@ -2039,9 +2040,21 @@ __global__ __launch_bounds__(64 * WAVES) void k_kv_evict(KvView c, const float *
         }
     });
     __syncthreads();
+    const int end = ahead ? c.blocks - (nb - stay) : stay;
+    if (ahead) {
+        if constexpr (KPT > 0) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                const int j = pick.place(i);
+                if (j >= nb && j < c.blocks) table_out[j - nb + stay] = page[i];
+            }
+        } else {
+            for (int j = nb + tid; j < c.blocks; j += 64 * WAVES) table_out[j - nb + stay] = table[j];
+        }
+    }
     for (int j = tid; j < c.blocks; j += 64 * WAVES) {
+        if (j >= end) table_out[j] = -1;
         if (j >= stay) {
-            table_out[j] = -1;
             mass_out[j] = j == stay && nb < c.blocks ? open : 0.f;
         }
         if (j >= nb - stay) freed[j] = -1;
