@@ -642,7 +642,7 @@ int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs,
  *           Rows of tokens that are no sequence's are left as they were
  *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes; any where that is 0
  * A row whose query, or of which a key that it sees, makes a logit +inf or not a number becomes not a number; a value that is not finite
- * makes its dimension so, in the rows that see it and in no other. */
+ * makes its dimension so, in the rows that see it and in no other.  Finite values, the type's largest too, give finite results. */
 int64_t etf_prompt_attend_workspace_bytes(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, int heads, int batch);
 int etf_prompt_attend(etf_ctx *ctx, int dtype, int head_dim, const void *q, const int64_t *q_strides, const void *k, const int64_t *k_strides, const void *v,
                       const int64_t *v_strides, int64_t tokens, int heads_q, int heads, const int32_t *starts, int batch, float scale, void *out, float *lse,

@@ -33,6 +33,10 @@ struct TBf {
     static __device__ __forceinline__ x2 narrow(float a, float b) { return __builtin_convertvector((f32x2){a, b}, x2); }
     static constexpr bool NARROW = false;
     static constexpr int UP = 0, TILE_UP = 0, TILE_LAG = 8;
+    // As large as float32's numbers: sums of weighted values may not be finite where their mean is one of the type's (k_prompt).
+    static constexpr bool WIDE = true;
+    static constexpr float MOST = 0x1.FEp127f;
+    static __device__ __forceinline__ void hold(float &) {}
 };
 struct THf {
     typedef f16x2 x2;
@@ -56,6 +60,15 @@ struct THf {
     // by 2^-39 of the largest at most (2^-31), besides its rounding.  2^10 and 2^4 in k_kv_tile: 135.7 instead of 134.7 us for pieces of
     // three prompts of up to 1000 tokens over caches of up to 10 001, 96 dimensions.
     static constexpr int UP = 14, TILE_UP = 6, TILE_LAG = 8;
+    static constexpr bool WIDE = false;
+    static constexpr float MOST = 65504.f;
+    // From here on what is rounded past the type's largest number becomes that one, infinities stay (FP16_OVFL, bit 23 of MODE).  What comes of f
+    // is worked out behind it.  No matrix product may follow: with it a query that is not a number gave ordinary results.
+    static __device__ __forceinline__ void hold(float &f)
+    {
+        __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);
+        asm volatile("" : "+v"(f));
+    }
 };
 
 // What weights 2^(z - reference) are taken against where `top` is the largest z: `up` bits below it.  Where float32 does not resolve

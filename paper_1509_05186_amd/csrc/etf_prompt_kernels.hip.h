@@ -54,6 +54,20 @@ struct PromptTile {
     static __device__ __forceinline__ int v_place(int token, int at) { return at ^ (D == 128 ? (token & 3) << 2 : D == 64 ? (token >> 1 & 1) << 2 : 0); }
 };
 
+// Rows whose sums of weighted values float32 does not hold have weights smaller by 2^prompt_down: a weight is 2^(TILE_UP + TILE_LAG) at most, so that
+// sums of as many as a row sees are no larger than its largest value.  Such a row's dimensions lose what is smaller than float32's smallest
+// normal number times that.
+template <typename T>
+__device__ __forceinline__ int prompt_down(int sees) { return T::TILE_UP + T::TILE_LAG + 32 - __builtin_clz(sees); }
+
+// o times f = 1 / l.  What rounded weights put past the type's largest number becomes that one.
+template <typename T>
+__device__ __forceinline__ float held_mean(float o, float f)
+{
+    const float x = o * f;
+    return fabsf(x) > T::MOST && fabsf(o) < INFINITY ? copysignf(T::MOST, x) : x;
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
 {
@@ -113,6 +127,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
 
     f32x16 o[DT];
     float m, l;
+    int down = 0;
     const int l16 = lane & 15, quad = l16 >> 2;
     const int v_at = (4 * half + quad) * D * 2 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;  // of the dimensions from 0 on, before exchange
     // four tokens from 16 u + 8 c + 4 half on of dimension 32 i + x
@@ -182,6 +197,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, -base));
+                if constexpr (T::WIDE && decltype(careful)::value) s[t][i] = __builtin_amdgcn_ldexpf(s[t][i], -down);
                 sum += s[t][i];
             }
         l += sum;
@@ -253,13 +269,17 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
         if (wlive && (j + 1) * KB < wmost) block(std::false_type(), j + 1, s_k1, s_v1);
     }
     // A value that is not finite makes whole tiles so, whether or not their rows see it, through products with weights of 0: such
-    // tiles are worked out again.
-    float zero = 0.f * l;
+    // tiles are worked out again.  Rows that are not finite then have such values themselves or sums that float32 does not hold: they
+    // are worked out once more, with smaller weights.
+    auto not_finite = [&]() __attribute__((always_inline)) {
+        float zero = 0.f * l;
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+        for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int y = 0; y < 16; ++y) zero = __builtin_fmaf(0.f, o[i][y], zero);
-    if (__syncthreads_or(valid && zero != 0.f)) {
+            for (int y = 0; y < 16; ++y) zero = __builtin_fmaf(0.f, o[i][y], zero);
+        return zero != 0.f;
+    };
+    auto once_more = [&]() __attribute__((always_inline)) {
         clear();
         for (int j = from; j < blocks; ++j) {
             load(j, s_k0, s_v0);
@@ -268,20 +288,42 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
             if (wlive && j * KB < wmost) block(std::true_type(), j, s_k0, s_v0);
             __syncthreads();
         }
+    };
+    if (__syncthreads_or(valid && not_finite())) {
+        once_more();
+        if constexpr (T::WIDE) {
+            int more = not_finite();
+            more |= __shfl_xor(more, 32);
+            if (more) down = prompt_down<T>(sees);
+            if (__syncthreads_or(valid && more)) once_more();
+            if (more) l = -l;  // tells that weights are smaller
+        }
     }
+    // the compiler keeps what follows apart for rows that come from here and from there, at 40 registers and more, unless something hides where they come from
+    if (T::WIDE) asm volatile("" : "+v"(l));
     l += __shfl_xor(l, 32);
     if (!valid) return;
 
     const int64_t at = (int64_t)(begin + qi) * H * g + h * g + hg;
     if (alone) {
-        const float f = 1.f / l;
+        float f = 1.f / fabsf(l);
+        T::hold(f);
+        uint16_t *to = a.out + at * D + 4 * half;
+        auto store = [&](auto mean) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
+            for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const typename T::x2 p0 = T::narrow(o[i][4 * y] * f, o[i][4 * y + 1] * f), p1 = T::narrow(o[i][4 * y + 2] * f, o[i][4 * y + 3] * f);
-                *reinterpret_cast<uint2 *>(a.out + at * D + 32 * i + 8 * y + 4 * half) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
-            }
+                for (int y = 0; y < 4; ++y) {
+                    const typename T::x2 p0 = T::narrow(mean(o[i][4 * y]), mean(o[i][4 * y + 1])), p1 = T::narrow(mean(o[i][4 * y + 2]), mean(o[i][4 * y + 3]));
+                    *reinterpret_cast<uint2 *>(to + 32 * i + 8 * y) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
+                }
+        };
+        if (T::WIDE && __any(l < 0.f)) {
+            store([&](float x) { return held_mean<T>(x, f); });
+            if (l < 0.f) l = __builtin_amdgcn_ldexpf(-l, prompt_down<T>(sees));
+        } else {
+            store([&](float x) { return x * f; });
+        }
         if (half == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
         return;
     }
@@ -312,16 +354,33 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a)
     float m = -INFINITY, l = 0.f;
     for (int s = 0; s < many; ++s) m = fmaxf(m, a.part_ml[(first + s * ROWS) * 2]);
     const float base = m == -INFINITY ? 0.f : m;
+    const float down = ldexpf(1.f, -prompt_down<T>((int)(row / g) + 1));
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < many; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (first + s * ROWS) * 2);
-        const float weight = __builtin_amdgcn_exp2f(ml.x - base);
-        l += ml.y * weight;
-        if (lane < D / 4) o += *reinterpret_cast<const f32x4 *>(a.part_o + (first + s * ROWS) * D + 4 * lane) * weight;
+    // `of`: the sums are of weights that are smaller by it
+    auto add = [&](float of) __attribute__((always_inline)) {
+        o = (f32x4){0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
+        for (int s = 0; s < many; ++s) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (first + s * ROWS) * 2);
+            float weight = __builtin_amdgcn_exp2f(ml.x - base);
+            if constexpr (T::WIDE) weight *= __builtin_signbit(ml.y) ? of / down : of;
+            l += fabsf(ml.y) * weight;
+            if (lane < D / 4) o += *reinterpret_cast<const f32x4 *>(a.part_o + (first + s * ROWS) * D + 4 * lane) * weight;
+        }
+    };
+    add(1.f);
+    const float lse = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    bool wide = false;
+    if constexpr (T::WIDE) {
+        wide = 0.f * o[0] + 0.f * o[1] + 0.f * o[2] + 0.f * o[3] != 0.f;
+        if (wide) add(down);
     }
-    const float f = 1.f / l;
+    float f = 1.f / l;
+    T::hold(f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = T::WIDE && wide ? held_mean<T>(o[i], f) : o[i] * f;
     const int64_t at = (int64_t)(begin + (int)(row / g)) * H * g + h * g + row % g;
-    const typename T::x2 p0 = T::narrow(o[0] * f, o[1] * f), p1 = T::narrow(o[2] * f, o[3] * f);
+    const typename T::x2 p0 = T::narrow(o[0], o[1]), p1 = T::narrow(o[2], o[3]);
     if (lane < D / 4) *reinterpret_cast<uint2 *>(a.out + at * D + 4 * lane) = make_uint2(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1));
-    if (lane == 0 && a.lse) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    if (lane == 0 && a.lse) a.lse[at] = lse;
 }
