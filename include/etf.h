@@ -551,8 +551,9 @@ int etf_kv_append(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const 
                   const int64_t *v_strides, int n, const int32_t *counts);
 
 /* The same for tokens that lie packed, one sequence's after the other's: sequence b's new tokens are [starts[b], starts[b + 1]) of
- * k, v [tokens][heads][head_dim] (starts: i32 [batch + 1], device, ascending, within [0, tokens]; counts as 0 or as tokens outside of
- * that, and a sequence whose end lies before its start has no new tokens).  strides[0..1]: elements from one token and head to the next. */
+ * k, v [tokens][heads][head_dim] (starts: i32 [batch + 1], device, within [0, tokens]; counts as 0 or as tokens outside of that.  They
+ * ascend; two equal ones: a sequence without new tokens.  Where they descend, nothing beyond the sequences' blocks is written, but which of
+ * them hold their new tokens is not defined).  strides[0..1]: elements from one token and head to the next. */
 int etf_kv_append_packed(etf_ctx *ctx, const etf_kv_cache *cache, const void *k, const int64_t *k_strides, const void *v, const int64_t *v_strides,
                          int64_t tokens, const int32_t *starts);
 
@@ -636,8 +637,8 @@ int etf_kv_compact(etf_ctx *ctx, const etf_kv_cache *cache, const int32_t *refs,
  *   q       16-bit [tokens][heads_q][head_dim]; k, v [tokens][heads][head_dim].  Rows lie at strides[0..1] = elements from one token
  *           and head to the next, multiples of 8, of tokens up to 2^23 (a NULL pointer: dense); a row is contiguous and 16-byte
  *           aligned.  Query head x reads key/value head x / (heads_q / heads)
- *   starts  i32 [batch + 1], device, ascending, within [0, tokens]; counts as 0 or as tokens outside of that.  A sequence of no tokens, or
- *           whose end lies before its start, has no rows
+ *   starts  i32 [batch + 1], device, within [0, tokens]; counts as 0 or as tokens outside of that.  They ascend; two equal ones: a sequence of no
+ *           tokens.  Where they descend, no row outside of [0, tokens) is read or written, but what the rows become is not defined
  *   out     dense [tokens][heads_q][head_dim], the rows' type; lse: NULL or float [tokens][heads_q].  Both share nothing with q, k, v.
  *           Rows of tokens that are no sequence's are left as they were
  *   ws      device, 256-byte aligned, at least etf_prompt_attend_workspace_bytes; any where that is 0

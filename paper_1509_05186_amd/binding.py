@@ -864,8 +864,8 @@ class Context:
         return mass_out, freed
 
     def kv_append_packed(self, cache: KvCache, k, v, starts):
-        """kv_append for packed tokens: k, v [tokens][H][D], sequence b's new ones are [starts[b], starts[b + 1]), starts int32 [B + 1]; the
-        caller then advances cache.lens.  There is no gradient."""
+        """kv_append for packed tokens: k, v [tokens][H][D], sequence b's new ones are [starts[b], starts[b + 1]), starts int32 [B + 1],
+        ascending; the caller then advances cache.lens.  There is no gradient."""
         import torch
         self._kv_here(cache)
         if k.requires_grad or v.requires_grad:
@@ -983,7 +983,7 @@ class Context:
 
     def prompt_attend(self, q, k, v, starts, scale: Optional[float] = None, out=None, lse=None, ws=None):
         """Causal attention of packed prompts: q [tokens][heads_q][D], k, v [tokens][heads][D], bfloat16 or float16; sequence b has the tokens
-        [starts[b], starts[b + 1]), starts int32 [B + 1].  scale: 1 / sqrt(D) by default; lse: float32 [tokens][heads_q], written if given.
+        [starts[b], starts[b + 1]), starts int32 [B + 1], ascending.  scale: 1 / sqrt(D) by default; lse: float32 [tokens][heads_q], written if given.
         Rows of tokens that are no sequence's are left as they were.  There is no gradient: tensors that require one are refused
         where torch would record it."""
         import torch

@@ -100,7 +100,7 @@ __device__ __forceinline__ typename T::x8 query8(typename T::x8 q)
     return __builtin_bit_cast(typename T::x8, w);
 }
 
-// Sequences that lie packed: sequence b has the tokens [starts[b], starts[b + 1]) of `tokens`.
+// Sequences that lie packed: sequence b has the tokens [starts[b], starts[b + 1]) of `tokens`; starts ascend.
 struct Packed {
     const int32_t *starts;
     int tokens, batch;
@@ -109,7 +109,8 @@ struct Packed {
 __device__ __forceinline__ int packed_start(const Packed &p, int b) { return min(max(p.starts[b], 0), p.tokens); }
 
 // All sequences share one numbering of tiles of ROWS rows, g rows to a token, that needs no counting: sequence b's tiles begin at number
-// floor(starts[b] g / ROWS) + b, since it has at most floor(n g / ROWS) + 1 of them.
+// floor(starts[b] g / ROWS) + b, since it has at most floor(n g / ROWS) + 1 of them.  Where starts descend, these overlap and a number may be another
+// sequence's: tiles are left out, but none is given to two numbers, and none is outside of its sequence.
 template <int ROWS>
 __device__ __forceinline__ int packed_base(const Packed &p, int b, int g) { return (int)((int64_t)packed_start(p, b) * g / ROWS) + b; }
 // The last sequence whose tiles begin at or before number `find`, or 0, by a search of 64 places at a time.  Every lane of the wave calls it.
