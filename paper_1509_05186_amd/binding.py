@@ -235,6 +235,17 @@ def _dev(t) -> int:
     return t.data_ptr()
 
 
+_ad = None    # torch.autograd.forward_ad, once a call has asked for it
+
+
+def _dual_level() -> bool:
+    """Whether tensors may carry tangents: within torch's dual_level() only, whose number torch keeps (-1 outside)."""
+    global _ad
+    if _ad is None:
+        import torch.autograd.forward_ad as _ad
+    return getattr(_ad, "_current_level", 0) >= 0
+
+
 class KvCache:
     """An attention cache in 8 bits: the device tensors of an etf_kv_cache, which the caller owns.
 
@@ -745,6 +756,8 @@ class Context:
             import torch
             if torch.is_grad_enabled():
                 raise ValueError("%s requires a gradient, and the cache calls have none: detach it, or call them under torch.no_grad()" % what)
+        if _dual_level() and _ad.unpack_dual(t).tangent is not None:    # torch.no_grad() leaves tangents on
+            raise ValueError("%s carries a tangent, and the cache calls have no derivative: detach it" % what)
 
     @staticmethod
     def _kv_dev(t, shape, dtype, cache: KvCache, what: str):
@@ -868,7 +881,7 @@ class Context:
         ascending; the caller then advances cache.lens.  There is no gradient."""
         import torch
         self._kv_here(cache)
-        if k.requires_grad or v.requires_grad:
+        if k.requires_grad or v.requires_grad or _dual_level():
             self._no_gradient(k, "k")
             self._no_gradient(v, "v")
         like, tokens = (cache.dtype, cache._gpu), k.shape[0]
@@ -987,7 +1000,7 @@ class Context:
         Rows of tokens that are no sequence's are left as they were.  There is no gradient: tensors that require one are refused
         where torch would record it."""
         import torch
-        if q.requires_grad or k.requires_grad or v.requires_grad:
+        if q.requires_grad or k.requires_grad or v.requires_grad or _dual_level():
             for t, what in ((q, "q"), (k, "k"), (v, "v")):
                 self._no_gradient(t, what)
         dtype, gpu, shape, of_k = q.dtype, q.get_device(), q.shape, k.shape
