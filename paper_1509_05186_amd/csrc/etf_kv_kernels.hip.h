@@ -40,14 +40,16 @@ __device__ __forceinline__ int64_t kv_tail(const KvView &c, int64_t bh, int b, i
 // Append.  A workgroup takes one block of one (sequence, head): where the new tokens complete it, it is sealed: the
 // smallest power of two s with amax <= 448 s, codes round_e4m3(x / s) (the division is exact), the values transposed
 // through LDS so that a row of a page is one dimension's 64 tokens, and every dimension's smallest and largest key code.
-// The workgroup of the first block also takes the open block's earlier tokens and writes what is left over into the open block, which may
-// lie in the same buffer: everything is read before anything is written.  Values of an open block lie by dimensions: eight tokens
-// to a load, and turned in LDS to a store where eight are left over.  A token that is not finite has keys that are not numbers
-// and values of zero: rows that see it become not a number, others do not.
-// Bound by vector issue and memory alike: four prompts of 8192 tokens, 8 heads of 128 dimensions (202 MB) 45 to 48 us = 4.2 to 4.5 TB/s; with maxima and
-// bounds number by number instead of two to an operation 53 us.  Packed prompts of 1617 to 4096 tokens (269 MB) 54 us = 5.0 TB/s, 63 with other
-// tensors each time.  Short calls are a chain of dependent steps: one token 2.2 us (with barriers and LDS 3.1), a block 6.0, a block of which 60 tokens were open and 60 are left over 9.9 (11.6 with the open
-// block's values read two bytes at a time and what is left over read twice).
+// The workgroup of the first block also takes the open block's earlier tokens and, once these are in registers, writes what is left over into the
+// open block, which may lie in the same buffer.  Values of an open block lie by dimensions: eight tokens to a load.  What is left over
+// goes there token by token where it is a few, and is turned in LDS first where it is more.  A token that is not finite has keys that are not
+// numbers and values of zero: rows that see it become not a number, others do not.
+// Bound by vector issue and memory alike: four prompts of 8192 tokens, 8 heads of 128 dimensions (202 MB) 46 us = 4.4 TB/s with other tensors each
+// time, 37 with the same; with maxima and bounds number by number instead of two to an operation 8 % more.  Packed prompts of 1617 to 4096 tokens (269 MB) 62 and 49 us = 4.3
+// and 5.5 TB/s.  Short calls are chains of dependent steps.  One sequence, 8 heads of 128 dimensions: one token 2.2 us and eight 2.6 (through barriers
+// and LDS 3.1 and 4.3), 24 tokens 4.3 (token by token in two rounds 4.0, but 512 sequences 21 and 32), a block 5.5, one of which 60 tokens were open
+// and 56 are left over 8.4 (9.0 with what is left over read ahead and written before the block is sealed, 13.6 with values read and written two bytes at a
+// time); 64 sequences with 200 tokens behind 10 open ones 27 us (30 and 29).
 // ------------------------------------------------------------------------------------------------
 struct KvAppendArgs {
     KvView c;
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     uint8_t *const s_v = s_all, *const s_k = s_all + D * VROW;
     static_assert(D * VROW % 16 == 0 && TROW >= KB && TROW % 2 == 0, "rows are aligned and hold a block");
     __shared__ uint32_t s_amax[2][4];
-    __shared__ int s_bad[2][KB];  // of the block that is sealed, of what is left over
+    __shared__ int s_bad[KB], s_some;  // tokens that are not finite; any of the open block's values
     constexpr int BW = D / 4, BG = 256 / BW, BT = (KB + BG - 1) / BG;  // bounds: words of a row, groups of tokens, tokens of a group
     __shared__ __attribute__((aligned(8))) int16_t s_edge[2][BG][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -130,37 +132,15 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
     const int first = len / KB, begin = len % KB;
     const int full = (begin + count) / KB, left = (begin + count) % KB;
     if (blk > 0 && blk >= full) return;
-    if (full == 0 && count * PT <= 64) {  // a few tokens into the open block: one wave, which needs no barrier
-        const int t = lane / PT, d = lane % PT * 8;
-        const bool mine = wave == 0 && t < count;
-        uint4 w = make_uint4(0, 0, 0, 0), u = w;
-        if (mine) {
-            w = *reinterpret_cast<const uint4 *>(nk + t * tk + d);
-            u = *reinterpret_cast<const uint4 *>(nv + t * tv + d);
-        }
-        const uint64_t bad = __ballot(max(size8(w), size8(u)) >= T::EXP);
-        if (!mine) return;
-        if (bad >> (t * PT) & ((1ull << PT) - 1)) {
-            constexpr uint32_t two = T::NOT | (uint32_t)T::NOT << 16;
-            w = make_uint4(two, two, two, two);
-            u = make_uint4(0, 0, 0, 0);
-        }
-        const int64_t now = kv_tail(a.c, bh, b, first, D);
-        *reinterpret_cast<uint4 *>(a.c.tail_k + now + (begin + t) * D + d) = w;
-        const uint32_t v[4] = {u.x, u.y, u.z, u.w};
-        for (int j = 0; j < 8; ++j) a.c.tail_v[now + (d + j) * KB + begin + t] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
-        return;
-    }
-    if (tid < KB) s_bad[0][tid] = s_bad[1][tid] = 0;
-    __syncthreads();
-    // all that the workgroup reads, asked for at once: the block's tokens, the open block's values as they lie, eight tokens of a dimension to a
-    // piece, and what is left over for the block that is open afterwards, tokens [from, left) of it
-    constexpr int OP = D * 8 / 256;
-    const bool seals = blk < full;
-    const int before = seals && blk == 0 ? begin : 0, from = full ? 0 : begin, over = blk == 0 ? left - from : 0;
+    const int before = blk < full && blk == 0 ? begin : 0, from = full ? 0 : begin, over = blk == 0 ? left - from : 0;
     const int64_t old = kv_tail(a.c, bh, b, first, D), now = kv_tail(a.c, bh, b, first + full, D);
-    uint4 kw[NP], vw[NP], ow[OP], lk[NP], lv[NP];
-    if (seals) {
+    if (blk < full) {
+        if (tid < KB) s_bad[tid] = 0;
+        if (tid == 0) s_some = 0;
+        __syncthreads();
+        // all that is sealed, asked for at once: the block's tokens, the open block's values as they lie, eight tokens of a dimension to a piece
+        constexpr int OP = D * 8 / 256;
+        uint4 kw[NP], vw[NP], ow[OP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
@@ -169,206 +149,227 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a)
             vw[i] = make_uint4(0, 0, 0, 0);
             if (at >= 0) vw[i] = *reinterpret_cast<const uint4 *>(nv + at * tv + d);
         }
-    }
-    if (before > 0) {
+        if (before > 0) {
 #pragma unroll
-        for (int i = 0; i < OP; ++i) {
-            const int p = tid + 256 * i, t0 = p % 8 * 8;
-            ow[i] = make_uint4(0, 0, 0, 0);
-            if (t0 < before) ow[i] = *reinterpret_cast<const uint4 *>(a.c.tail_v + old + p / 8 * KB + t0);
+            for (int i = 0; i < OP; ++i) {
+                const int p = tid + 256 * i, t0 = p % 8 * 8;
+                ow[i] = make_uint4(0, 0, 0, 0);
+                if (t0 < before) ow[i] = *reinterpret_cast<const uint4 *>(a.c.tail_v + old + p / 8 * KB + t0);
+            }
         }
-    }
-    if (over > 0) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
-            if (t >= over) continue;
-            const int at = full * KB + from + t - begin;
-            lk[i] = *reinterpret_cast<const uint4 *>(nk + at * tk + d);
-            lv[i] = *reinterpret_cast<const uint4 *>(nv + at * tv + d);
-        }
-    }
-    // tokens that are not finite
-    uint32_t ks[NP], vs[NP];
-    bool some = false;
-    if (seals) {
+        // tokens that are not finite
+        uint32_t ks[NP], vs[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             ks[i] = size8(kw[i]);
             vs[i] = size8(vw[i]);
-            if (max(ks[i], vs[i]) >= T::EXP) s_bad[0][(tid + 256 * i) / PT] = 1;
+            if (max(ks[i], vs[i]) >= T::EXP) s_bad[(tid + 256 * i) / PT] = 1;
         }
-    }
-    if (before > 0) {
+        if (before > 0) {
 #pragma unroll
-        for (int i = 0; i < OP; ++i) {
-            const int t0 = (tid + 256 * i) % 8 * 8, have = before - t0;
-            auto first = [&](uint32_t u, int at) { return have >= at + 2 ? u : have > at ? u & 0xFFFFu : 0u; };
-            ow[i] = make_uint4(first(ow[i].x, 0), first(ow[i].y, 2), first(ow[i].z, 4), first(ow[i].w, 6));
-            if (size8(ow[i]) < T::EXP) continue;
-            some = true;
-            const uint32_t u[4] = {ow[i].x, ow[i].y, ow[i].z, ow[i].w};
-            for (int j = 0; j < 8; ++j)
-                if ((u[j / 2] >> (16 * (j & 1)) & T::EXP) == T::EXP) s_bad[0][t0 + j] = 1;
+            for (int i = 0; i < OP; ++i) {
+                const int t0 = (tid + 256 * i) % 8 * 8, have = before - t0;
+                auto first = [&](uint32_t u, int at) { return have >= at + 2 ? u : have > at ? u & 0xFFFFu : 0u; };
+                ow[i] = make_uint4(first(ow[i].x, 0), first(ow[i].y, 2), first(ow[i].z, 4), first(ow[i].w, 6));
+                if (size8(ow[i]) < T::EXP) continue;
+                s_some = 1;
+                const uint32_t u[4] = {ow[i].x, ow[i].y, ow[i].z, ow[i].w};
+                for (int j = 0; j < 8; ++j)
+                    if ((u[j / 2] >> (16 * (j & 1)) & T::EXP) == T::EXP) s_bad[t0 + j] = 1;
+            }
         }
-    }
-    if (over > 0) {
+        __syncthreads();  // the open block's tokens, whose buffer may be the one that is open afterwards, are in registers
+        uint32_t mk = 0, mv = 0;
+        if (before > 0) {
+#pragma unroll
+            for (int i = 0; i < OP; ++i) {
+                if (s_some) {
+                    const int t0 = (tid + 256 * i) % 8 * 8;
+                    auto fine = [&](uint32_t u, int at) { return (s_bad[t0 + at] ? 0u : u & 0xFFFFu) | (s_bad[t0 + at + 1] ? 0u : u & 0xFFFF0000u); };
+                    ow[i] = make_uint4(fine(ow[i].x, 0), fine(ow[i].y, 2), fine(ow[i].z, 4), fine(ow[i].w, 6));
+                }
+                mv = max(mv, size8(ow[i]));
+            }
+        }
+        bool bad[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int t = (tid + 256 * i) / PT;
-            if (t < over && max(size8(lk[i]), size8(lv[i])) >= T::EXP) s_bad[1][t] = 1;
+            bad[i] = s_bad[(tid + 256 * i) / PT] != 0;
+            if (!bad[i]) {
+                mk = max(mk, ks[i]);
+                mv = max(mv, vs[i]);
+            }
         }
-    }
-    some = __syncthreads_or(some);
-    if (over > 0) {
-        // what is left over; the open block's tokens, which may lie in the same buffer, are in registers
-        const bool many = over >= 8;  // then values are turned in LDS and written eight tokens at a time
-        uint16_t *s_t = reinterpret_cast<uint16_t *>(s_all);
+        for (int o = 32; o; o >>= 1) {
+            mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
+            mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
+        }
+        if (lane == 0) {
+            s_amax[0][wave] = mk;
+            s_amax[1][wave] = mv;
+        }
+        __syncthreads();
+        const int ek = scale_exponent(T::wide((uint16_t)max(max(s_amax[0][0], s_amax[0][1]), max(s_amax[0][2], s_amax[0][3]))));
+        const int ev = scale_exponent(T::wide((uint16_t)max(max(s_amax[1][0], s_amax[1][1]), max(s_amax[1][2], s_amax[1][3]))));
+        const float ik = ldexpf(1.f, -ek), iv = ldexpf(1.f, -ev);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
-            if (t >= over) continue;
-            if (s_bad[1][t]) {
-                constexpr uint32_t two = T::NOT | (uint32_t)T::NOT << 16;
-                lk[i] = make_uint4(two, two, two, two);
-                lv[i] = make_uint4(0, 0, 0, 0);
+            uint2 ck = codes8<T>(kw[i], ik), cv = codes8<T>(vw[i], iv);
+            if (bad[i]) {
+                ck = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                cv = make_uint2(0, 0);
             }
-            *reinterpret_cast<uint4 *>(a.c.tail_k + now + (from + t) * D + d) = lk[i];
-            const uint32_t w[4] = {lv[i].x, lv[i].y, lv[i].z, lv[i].w};
-            for (int j = 0; j < 8; ++j) {
-                const uint16_t u = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-                if (many) s_t[(d + j) * TROW + from + t] = u;
-                else a.c.tail_v[now + (d + j) * KB + from + t] = u;
-            }
+            *reinterpret_cast<uint2 *>(s_k + t * D + d) = ck;
+            if (t >= before)
+                for (int j = 0; j < 8; ++j) s_v[(d + j) * VROW + t] = (uint8_t)((j < 4 ? cv.x : cv.y) >> (8 * (j & 3)));
         }
-        if (many) {
-            __syncthreads();
-            for (int p = tid; p < D * 8; p += 256) {
-                const int d = p / 8, t0 = p % 8 * 8, lo = max(from - t0, 0), hi = min(left - t0, 8);  // of the piece's tokens, those that are new
-                if (lo >= hi) continue;
-                uint32_t w[4];
-                uint4 *to = reinterpret_cast<uint4 *>(a.c.tail_v + now + d * KB + t0);
-                for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t *>(s_t + d * TROW + t0 + 2 * j);
-                if (lo > 0 || hi < 8) {
-                    const uint4 was = *to;
-                    const uint32_t o[4] = {was.x, was.y, was.z, was.w};
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t take = (2 * j >= lo && 2 * j < hi ? 0xFFFFu : 0u) | (2 * j + 1 >= lo && 2 * j + 1 < hi ? 0xFFFF0000u : 0u);
-                        w[j] = (w[j] & take) | (o[j] & ~take);
-                    }
+        if (before > 0) {
+#pragma unroll
+            for (int i = 0; i < OP; ++i) {
+                const int p = tid + 256 * i, t0 = p % 8 * 8, have = min(8, before - t0);
+                const uint2 cv = codes8<T>(ow[i], iv);
+                uint8_t *to = s_v + p / 8 * VROW + t0;
+                if (have == 8) {
+                    reinterpret_cast<uint32_t *>(to)[0] = cv.x;
+                    reinterpret_cast<uint32_t *>(to)[1] = cv.y;
+                } else {
+                    for (int j = 0; j < have; ++j) to[j] = (uint8_t)((j < 4 ? cv.x : cv.y) >> (8 * (j & 3)));
                 }
-                *to = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            __syncthreads();
         }
-    }
-    if (!seals) return;
-    uint32_t mk = 0, mv = 0;
-    if (before > 0) {
-#pragma unroll
-        for (int i = 0; i < OP; ++i) {
-            if (some) {
-                const int t0 = (tid + 256 * i) % 8 * 8;
-                auto fine = [&](uint32_t u, int at) { return (s_bad[0][t0 + at] ? 0u : u & 0xFFFFu) | (s_bad[0][t0 + at + 1] ? 0u : u & 0xFFFF0000u); };
-                ow[i] = make_uint4(fine(ow[i].x, 0), fine(ow[i].y, 2), fine(ow[i].z, 4), fine(ow[i].w, 6));
+        __syncthreads();
+        const int page = kv_page(a.c, bh, first + blk);
+        if (page >= 0) {
+            for (int p = tid; p < KB * D / 16; p += 256) {
+                reinterpret_cast<uint4 *>(a.c.k + (int64_t)page * (KB * D))[p] = reinterpret_cast<const uint4 *>(s_k)[p];
+                const uint32_t *r = reinterpret_cast<const uint32_t *>(s_v + p / 4 * VROW + p % 4 * 16);
+                reinterpret_cast<uint4 *>(a.c.v + (int64_t)page * (KB * D))[p] = make_uint4(r[0], r[1], r[2], r[3]);
             }
-            mv = max(mv, size8(ow[i]));
-        }
-    }
-    bool bad[NP];
+            // smallest and largest codes: four dimensions and a group of tokens to a thread, then the groups
+            if (tid < BW * BG) {
+                const int w = tid % BW, grp = tid / BW;
+                i16x2 lo[2], hi[2];  // of bytes 0 and 2, of bytes 1 and 3
+                lo[0] = lo[1] = 0x7F;
+                hi[0] = hi[1] = -0x80;
+                for (int t = grp * BT; t < min(KB, (grp + 1) * BT); ++t) {
+                    if (s_bad[t]) continue;
+                    const i16x2 u = *reinterpret_cast<const i16x2 *>(s_k + t * D + 4 * w);
+                    const i16x2 even = code_order((i16x2)(u << 8) >> 8), odd = code_order(u >> 8);
+                    lo[0] = __builtin_elementwise_min(lo[0], even);
+                    lo[1] = __builtin_elementwise_min(lo[1], odd);
+                    hi[0] = __builtin_elementwise_max(hi[0], even);
+                    hi[1] = __builtin_elementwise_max(hi[1], odd);
+                }
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        bad[i] = s_bad[0][(tid + 256 * i) / PT] != 0;
-        if (!bad[i]) {
-            mk = max(mk, ks[i]);
-            mv = max(mv, vs[i]);
+                for (int i = 0; i < 4; ++i) {
+                    s_edge[0][grp][4 * w + i] = lo[i & 1][i >> 1];
+                    s_edge[1][grp][4 * w + i] = hi[i & 1][i >> 1];
+                }
+            }
+            if (tid < 2) a.c.scales[(int64_t)page * 2 + tid] = ldexpf(1.f, tid ? ev : ek);
+        }
+        __syncthreads();
+        if (page >= 0 && tid < 2 * BW) {
+            const int e = tid / BW, d = tid % BW * 4;
+            uint32_t out = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int lo = 0x7F, hi = -0x80;
+                for (int y = 0; y < BG; ++y) {
+                    lo = min(lo, (int)s_edge[0][y][d + i]);
+                    hi = max(hi, (int)s_edge[1][y][d + i]);
+                }
+                const i16x2 o = {(int16_t)(lo > hi ? 0 : e ? hi : lo), 0};
+                const uint32_t code = (uint32_t)(uint16_t)code_order(o)[0] & 0xFF;
+                out |= (code == 0x80 ? 0 : code) << (8 * i);  // no -0
+            }
+            *reinterpret_cast<uint32_t *>(a.c.bounds + ((int64_t)page * 2 + e) * D + d) = out;
         }
     }
-    for (int o = 32; o; o >>= 1) {
-        mk = max(mk, (uint32_t)__shfl_xor((int)mk, o));
-        mv = max(mv, (uint32_t)__shfl_xor((int)mv, o));
+    // what is left over, tokens [from, left) of the block that is open afterwards
+    if (over <= 0) return;
+    constexpr uint32_t two = T::NOT | (uint32_t)T::NOT << 16;
+    const int64_t new0 = full * KB + from - begin;  // the first of them among the new tokens
+    constexpr int TW = 64 / PT;
+    if (over <= 4 * TW) {  // a few: whole tokens to a wave, which need no barrier
+        const int t = wave * TW + lane / PT, d = lane % PT * 8;
+        const bool mine = lane < TW * PT && t < over;
+        uint4 w = make_uint4(0, 0, 0, 0), u = w;
+        if (mine) {
+            w = *reinterpret_cast<const uint4 *>(nk + (new0 + t) * tk + d);
+            u = *reinterpret_cast<const uint4 *>(nv + (new0 + t) * tv + d);
+        }
+        const uint64_t bad = __ballot(max(size8(w), size8(u)) >= T::EXP);
+        if (!mine) return;
+        if (bad >> (lane / PT * PT) & ((1ull << PT) - 1)) {
+            w = make_uint4(two, two, two, two);
+            u = make_uint4(0, 0, 0, 0);
+        }
+        *reinterpret_cast<uint4 *>(a.c.tail_k + now + (from + t) * D + d) = w;
+        const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+        for (int j = 0; j < 8; ++j) a.c.tail_v[now + (d + j) * KB + from + t] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
+        return;
     }
-    if (lane == 0) {
-        s_amax[0][wave] = mk;
-        s_amax[1][wave] = mv;
-    }
-    __syncthreads();
-    const int ek = scale_exponent(T::wide((uint16_t)max(max(s_amax[0][0], s_amax[0][1]), max(s_amax[0][2], s_amax[0][3]))));
-    const int ev = scale_exponent(T::wide((uint16_t)max(max(s_amax[1][0], s_amax[1][1]), max(s_amax[1][2], s_amax[1][3]))));
-    const float ik = ldexpf(1.f, -ek), iv = ldexpf(1.f, -ev);
+    // more: values are turned in LDS and written eight tokens at a time, at the ends four, two and one
+    uint4 lk[NP], lv[NP];
+    if (tid < KB) s_bad[tid] = 0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
-        uint2 ck = codes8<T>(kw[i], ik), cv = codes8<T>(vw[i], iv);
-        if (bad[i]) {
-            ck = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
-            cv = make_uint2(0, 0);
-        }
-        *reinterpret_cast<uint2 *>(s_k + t * D + d) = ck;
-        if (t >= before)
-            for (int j = 0; j < 8; ++j) s_v[(d + j) * VROW + t] = (uint8_t)((j < 4 ? cv.x : cv.y) >> (8 * (j & 3)));
-    }
-    if (before > 0) {
-#pragma unroll
-        for (int i = 0; i < OP; ++i) {
-            const int p = tid + 256 * i, t0 = p % 8 * 8, have = min(8, before - t0);
-            const uint2 cv = codes8<T>(ow[i], iv);
-            uint8_t *to = s_v + p / 8 * VROW + t0;
-            if (have == 8) {
-                reinterpret_cast<uint32_t *>(to)[0] = cv.x;
-                reinterpret_cast<uint32_t *>(to)[1] = cv.y;
-            } else {
-                for (int j = 0; j < have; ++j) to[j] = (uint8_t)((j < 4 ? cv.x : cv.y) >> (8 * (j & 3)));
-            }
-        }
+        if (t >= over) continue;
+        lk[i] = *reinterpret_cast<const uint4 *>(nk + (new0 + t) * tk + d);
+        lv[i] = *reinterpret_cast<const uint4 *>(nv + (new0 + t) * tv + d);
     }
     __syncthreads();
-    const int page = kv_page(a.c, bh, first + blk);
-    if (page >= 0) {
-        for (int p = tid; p < KB * D / 16; p += 256) {
-            reinterpret_cast<uint4 *>(a.c.k + (int64_t)page * (KB * D))[p] = reinterpret_cast<const uint4 *>(s_k)[p];
-            const uint32_t *r = reinterpret_cast<const uint32_t *>(s_v + p / 4 * VROW + p % 4 * 16);
-            reinterpret_cast<uint4 *>(a.c.v + (int64_t)page * (KB * D))[p] = make_uint4(r[0], r[1], r[2], r[3]);
-        }
-        // smallest and largest codes: four dimensions and a group of tokens to a thread, then the groups
-        if (tid < BW * BG) {
-            const int w = tid % BW, grp = tid / BW;
-            i16x2 lo[2], hi[2];  // of bytes 0 and 2, of bytes 1 and 3
-            lo[0] = lo[1] = 0x7F;
-            hi[0] = hi[1] = -0x80;
-            for (int t = grp * BT; t < min(KB, (grp + 1) * BT); ++t) {
-                if (s_bad[0][t]) continue;
-                const i16x2 u = *reinterpret_cast<const i16x2 *>(s_k + t * D + 4 * w);
-                const i16x2 even = code_order((i16x2)(u << 8) >> 8), odd = code_order(u >> 8);
-                lo[0] = __builtin_elementwise_min(lo[0], even);
-                lo[1] = __builtin_elementwise_min(lo[1], odd);
-                hi[0] = __builtin_elementwise_max(hi[0], even);
-                hi[1] = __builtin_elementwise_max(hi[1], odd);
-            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s_edge[0][grp][4 * w + i] = lo[i & 1][i >> 1];
-                s_edge[1][grp][4 * w + i] = hi[i & 1][i >> 1];
-            }
-        }
-        if (tid < 2) a.c.scales[(int64_t)page * 2 + tid] = ldexpf(1.f, tid ? ev : ek);
+    for (int i = 0; i < NP; ++i) {
+        const int t = (tid + 256 * i) / PT;
+        if (t < over && max(size8(lk[i]), size8(lv[i])) >= T::EXP) s_bad[t] = 1;
     }
     __syncthreads();
-    if (page >= 0 && tid < 2 * BW) {
-        const int e = tid / BW, d = tid % BW * 4;
-        uint32_t out = 0;
+    uint16_t *s_t = reinterpret_cast<uint16_t *>(s_all);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int lo = 0x7F, hi = -0x80;
-            for (int y = 0; y < BG; ++y) {
-                lo = min(lo, (int)s_edge[0][y][d + i]);
-                hi = max(hi, (int)s_edge[1][y][d + i]);
-            }
-            const i16x2 o = {(int16_t)(lo > hi ? 0 : e ? hi : lo), 0};
-            const uint32_t code = (uint32_t)(uint16_t)code_order(o)[0] & 0xFF;
-            out |= (code == 0x80 ? 0 : code) << (8 * i);  // no -0
+    for (int i = 0; i < NP; ++i) {
+        const int p = tid + 256 * i, t = p / PT, d = p % PT * 8;
+        if (t >= over) continue;
+        if (s_bad[t]) {
+            lk[i] = make_uint4(two, two, two, two);
+            lv[i] = make_uint4(0, 0, 0, 0);
         }
-        *reinterpret_cast<uint32_t *>(a.c.bounds + ((int64_t)page * 2 + e) * D + d) = out;
+        *reinterpret_cast<uint4 *>(a.c.tail_k + now + (from + t) * D + d) = lk[i];
+        const uint32_t w[4] = {lv[i].x, lv[i].y, lv[i].z, lv[i].w};
+        for (int j = 0; j < 8; ++j) s_t[(d + j) * TROW + from + t] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+    }
+    __syncthreads();
+    for (int p = tid; p < D * 8; p += 256) {
+        const int d = p / 8, t0 = p % 8 * 8, lo = max(from - t0, 0), hi = min(left - t0, 8);  // of the piece's tokens, those that are new
+        if (lo >= hi) continue;
+        const uint16_t *of = s_t + d * TROW + t0;
+        uint16_t *to = a.c.tail_v + now + d * KB + t0;
+        auto pair = [&](int j) { return *reinterpret_cast<const uint32_t *>(of + j); };
+        if (hi - lo == 8) {
+            *reinterpret_cast<uint4 *>(to) = make_uint4(pair(0), pair(2), pair(4), pair(6));
+            continue;
+        }
+        int j = lo;
+        if (j & 1) {
+            to[j] = of[j];
+            ++j;
+        }
+        if ((j & 2) && j + 2 <= hi) {
+            *reinterpret_cast<uint32_t *>(to + j) = pair(j);
+            j += 2;
+        }
+        if (!(j & 3) && j + 4 <= hi) {
+            *reinterpret_cast<uint2 *>(to + j) = make_uint2(pair(j), pair(j + 2));
+            j += 4;
+        }
+        if (j + 2 <= hi) {
+            *reinterpret_cast<uint32_t *>(to + j) = pair(j);
+            j += 2;
+        }
+        if (j < hi) to[j] = of[j];
     }
 }
 

@@ -32,8 +32,25 @@ def equal(x, y):
 @pytest.mark.parametrize("bad", [False, True])
 def test_every_place_and_both_buffers(dtype, D, H, evicted, bad):
     say("append", dtype, D, H, "evicted", evicted, "bad", bad)
-    lens, counts = (list(x) for x in zip(*CASES))
-    B = len(CASES)
+    check(CASES, dtype, D, H, evicted, bad)
+
+
+@pytest.mark.parametrize("dtype,D,H", [(BF, 128, 1), (HF, 96, 2), (BF, 64, 1)])
+@pytest.mark.parametrize("sealed", [0, 1, 2])
+def test_both_sides_of_a_few_tokens(dtype, D, H, sealed):
+    """What is left over is written token by token up to 16, 20 and 32 of them (128, 96 and 64 dimensions), and turned first from there on; at every
+    place in its block that pieces of eight tokens begin or end."""
+    say("a few", dtype, D, H, sealed)
+    few = {128: 16, 96: 20, 64: 32}[D]
+    over = [few - 1, few, few + 1, few + 2, few + 5, few + 9]
+    cases = [(61, 3 + 64 * (sealed - 1) + n) for n in over + [63]] if sealed else [(begin, n) for n in over for begin in (0, 1, 2, 3, 5, 6, 7, 8, 17, 22)]
+    for bad in (False, True):
+        check(cases, dtype, D, H, 1, bad)
+
+
+def check(cases, dtype, D, H, evicted, bad):
+    lens, counts = (list(x) for x in zip(*cases))
+    B = len(cases)
     g = torch.Generator().manual_seed(D + evicted)
     made = lambda n: [torch.randn(B, n, H, D, generator=g).to(dtype) for _ in range(2)]  # noqa: E731
 
