@@ -559,7 +559,8 @@ int etf_kv_append_packed(etf_ctx *ctx, const etf_kv_cache *cache, const void *k,
 
 /* Attention over the cache: with s = scale * <q, k_t> over the tokens that a row sees, out = sum softmax(s)_t v_t (dense
  * [batch][n][heads_q][head_dim], the cache's type) and, where lse is not NULL, lse = log sum exp(s) (float [batch][n][heads_q]).
- * Sums, maxima and products are float32; weights are rounded to the cache's type for their product with the values.
+ * Sums, maxima and products are float32; weights are rounded to the cache's type for their product with the values.  The sums are
+ * not normalised, of weights up to 2^8: values that make 2^8 |v| times the tokens pass float32's range (bf16 only) may give infinities.
  *   lists  NULL: all tokens.  Else i32 [batch][n][heads][w] (etf_kv_select's): a token sees only these blocks of the ones
  *          that it sees as a whole (entries that are none of these are passed over; a block stands there once at
  *          most), and the tokens up to itself of the block that it lies in

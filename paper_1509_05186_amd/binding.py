@@ -323,7 +323,8 @@ class KvCache:
                    zeros(batch, heads, 2, head_dim, S, dtype=dtype), table, zeros(batch, dtype=torch.int32), zeros(batch, dtype=torch.int32))
 
     def fork(self) -> "KvCache":
-        """Another table, lens and evicted (uninitialised) over the same pages and open blocks, for Context.kv_evict to write."""
+        """Another table, lens and evicted (uninitialised) over the same pages and open blocks, for Context.kv_evict to write.
+        Not a copy of its sequences: that is Context.kv_fork."""
         import torch
         new = KvCache.__new__(KvCache)
         new.__dict__.update(self.__dict__)

@@ -14,7 +14,7 @@ namespace {
 
 #include "etf_prompt_kernels.hip.h"
 
-constexpr int64_t PROMPT_FEW = 768;    // (tile, head) units from which the card is full without ranges: it holds 512 workgroups at once
+constexpr int64_t PROMPT_FEW = 768;    // (tile, head) units from which the card is full without ranges: it holds 512 workgroups of 128 dimensions at once, 768 of 64 and 96
 constexpr int64_t PROMPT_LEAST = 8;    // blocks of a range, at least
 constexpr int64_t PROMPT_RANGES = 16;  // ranges of a tile, at most
 
@@ -52,8 +52,9 @@ int plan_prompt(const etf_ctx *ctx, int head_dim, int64_t tokens, int heads_q, i
     // Few tiles do not fill the card, and the longest of them decides: their blocks are cut into ranges of `per`.  What that costs is the ranges' partial
     // results, written and read again, about as much as 1 / 35 of a block's time for each of them, and the launch that joins them, four blocks':
     // per blocks and units * longest / (2 per) partial results take the least together where both are sqrt(units * longest / 70).  The
-    // host knows the number of tokens, not the lengths: of several prompts the longest is taken to be twice the mean.
-    // One prompt, 128 dimensions: 4096 tokens, 2 heads 79 us uncut, 38 cut; 8000 tokens, 1 head 145 and 45; 8 heads, four query heads to each:
+    // host knows the number of tokens, not the lengths: of several prompts the longest is taken to be twice the mean (one of 8000 tokens, 1 head, beside 15 of one
+    // token is left uncut, 144 us).  Measured with 128 dimensions, for all.
+    // One prompt, 128 dimensions: 4096 tokens, 2 heads 79 us uncut, 38 cut; 8000 tokens, 1 head 145 and 45 to 51; 8 heads, four query heads to each:
     // 600 tokens 20 and 25, 1000 tokens 28 and 36, 2000 tokens 51 and 72, which are left uncut.
     const int64_t units = p.tiles * heads, blocks = (tokens + KB - 1) / KB, longest = batch == 1 ? blocks : std::min(blocks, 2 * ((blocks + batch - 1) / batch));
     const int64_t per = std::max<int64_t>(PROMPT_LEAST, (int64_t)std::sqrt(units * longest / 70.));

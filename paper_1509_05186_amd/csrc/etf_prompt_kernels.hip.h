@@ -76,7 +76,8 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs a)
     __shared__ __attribute__((aligned(1024))) uint8_t s_k0[KB * D * 2], s_v0[KB * D * 2], s_k1[KB * D * 2], s_v1[KB * D * 2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, half = lane >> 5;
     const int H = a.heads, g = a.g;
-    // A prompt's last tiles, the longest ones, first; where all workgroups run at once, two to a compute unit, the second ones from the other end, so that
+    // A prompt's last tiles, the longest ones, first; where all workgroups run at once, two to a compute unit (of 64 and 96 dimensions it holds three; the
+    // limit is that of 128, with which it was measured), the second ones from the other end, so that
     // a long tile has a short one beside it (two prompts of 950 tokens, 8 heads, four query heads to each: 32 us instead of 36; one of 2000: 50 instead of 51).
     // Cutting a tile's blocks between two groups of waves of a larger workgroup as well: 25 us instead of 27 for 1000 tokens, nothing for 600 and
     // 1500; left out, since a row's sums would then depend on the call that it is in.
